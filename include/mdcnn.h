@@ -59,7 +59,7 @@ typedef enum {
     MDCNN_ERR_HIP = 7      /* a HIP launch failed; see mdcnn_last_error()        */
 } mdcnn_status;
 
-typedef enum { MDCNN_F32 = 0, MDCNN_F16 = 1 } mdcnn_dtype;
+typedef enum { MDCNN_F32 = 0, MDCNN_F16 = 1, MDCNN_BF16 = 2 /* operators behind the maps only */ } mdcnn_dtype;
 typedef enum { MDCNN_SITE_INPUT = 0, MDCNN_SITE_PREACT = 1, MDCNN_SITE_OUTPUT = 2 } mdcnn_site_kind;
 
 /* Description of one site.  INPUT sites hold A only, OUTPUT sites hold P only. */
@@ -600,6 +600,48 @@ mdcnn_status mdcnn_profile_read_launches(int cap, int* cls, int* site, int* edge
  * floating-point operations of the launch; sink_dev: at least one float of device memory. */
 mdcnn_status mdcnn_bench_copy(const void* src_dev, void* dst_dev, size_t bytes, void* stream);
 mdcnn_status mdcnn_bench_mfma(int iters, int blocks, float* sink_dev, void* stream, double* flops);
+
+/* ---- Operators behind the feature maps: reading a memory of past frames -------------------------------------------------
+ *
+ * A video model does not end with the map of a frame: its channels are normalised, turned by where and when their pixel was
+ * seen, put into a memory that outlives the frame, and that memory is read for the next one.  These calls do that on the GPU
+ * behind the calls above, under the same conventions: device memory is the caller's, nothing is allocated, read back or waited
+ * for, errors are found before anything is enqueued.  Storage is f32, f16 or bf16 (MDCNN_BF16), arithmetic fp32 with one rounding per stored
+ * value.  Workspaces hold nothing from one call to the next; calls on different streams need workspaces of their own. */
+
+/* Elements between images, rows and pixels of a map; its channels lie side by side.  Maps that are read may have any strides >= 0,
+ * maps that are written no two pixels in one place. */
+typedef struct { long long n, y, x; } mdcnn_strides;
+
+typedef enum { MDCNN_ACT_NONE = 0, MDCNN_ACT_RELU = 1, MDCNN_ACT_SILU = 2 } mdcnn_act;
+
+/* Group norm with an activation over N maps of H x W pixels and C channels (1 <= C <= 4096, a multiple of groups; N >= 0):
+ *   z = (x - mean) rstd,  y = act(gamma z + beta),  rstd = 1 / sqrt(variance + eps)
+ * with mean and (biased) variance over the H W C / groups values of an image and group. */
+typedef struct {
+    int N, H, W, C, groups;
+    int dtype;                /* of x, y, dy and dx                                     */
+    int act;                  /* mdcnn_act                                              */
+    float eps;                /* >= 0                                                   */
+    const float* gamma_dev;   /* C floats, or NULL: ones                                */
+    const float* beta_dev;    /* C floats, or NULL: zeros                               */
+    mdcnn_strides xs;         /* of x                                                   */
+    mdcnn_strides ys;         /* of y; of dx in the backward call                       */
+    mdcnn_strides ds;         /* of dy (backward call only)                             */
+} mdcnn_group_norm_desc;
+/* Workspace of the forward (backward = 0) or backward call, in bytes (may be 0). */
+mdcnn_status mdcnn_group_norm_bytes(const mdcnn_group_norm_desc* d, int backward, size_t* bytes);
+/* y_dev <- the above; mean_dev, rstd_dev: N * groups floats each, always written.  y_dev may be x_dev with the same strides. */
+mdcnn_status mdcnn_group_norm(const mdcnn_group_norm_desc* d, const void* x_dev, void* y_dev,
+                              float* mean_dev, float* rstd_dev, void* work_dev, size_t work_bytes,
+                              void* stream);
+/* Gradients from dy_dev and what the forward call left in mean_dev and rstd_dev: dx_dev, and dgamma_dev, dbeta_dev (C floats
+ * each, written even for N = 0).  No atomics: the same inputs give the same bits.  dx_dev may be dy_dev or x_dev with
+ * the same strides. */
+mdcnn_status mdcnn_group_norm_backward(const mdcnn_group_norm_desc* d, const void* x_dev, const void* dy_dev,
+                                       const float* mean_dev, const float* rstd_dev, void* dx_dev,
+                                       float* dgamma_dev, float* dbeta_dev, void* work_dev,
+                                       size_t work_bytes, void* stream);
 
 const char* mdcnn_last_error(void);
 const char* mdcnn_version(void);

@@ -14,7 +14,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmdcnn.so")
 
 MDCNN_OK = 0
-MDCNN_F32, MDCNN_F16 = 0, 1
+MDCNN_F32, MDCNN_F16, MDCNN_BF16 = 0, 1, 2
+MDCNN_ACT_NONE, MDCNN_ACT_RELU, MDCNN_ACT_SILU = 0, 1, 2
 MDCNN_SITE_INPUT, MDCNN_SITE_PREACT, MDCNN_SITE_OUTPUT = 0, 1, 2
 (MDCNN_VIEW_A, MDCNN_VIEW_P, MDCNN_VIEW_DELTA, MDCNN_VIEW_FLAGS, MDCNN_VIEW_LIST,
  MDCNN_VIEW_CLIST, MDCNN_VIEW_STATS, MDCNN_VIEW_OUT, MDCNN_VIEW_POOL_PREV, MDCNN_VIEW_CROP_OUT,
@@ -31,7 +32,7 @@ STATUS_NAMES = {0: "OK", 1: "ERR_NULL", 2: "ERR_SHAPE", 3: "ERR_DTYPE", 4: "ERR_
 EXPORTS = ["mdcnn_conv_border", "mdcnn_conv_tiles", "mdcnn_rect_tiles", "mdcnn_gather_tile", "mdcnn_buffer_bytes", "mdcnn_create_buffer", "mdcnn_destroy_buffer",
            "mdcnn_shift_camera", "mdcnn_set_crop", "mdcnn_layer_forward", "mdcnn_layer_forward_noalloc", "mdcnn_net_create", "mdcnn_net_destroy",
            "mdcnn_frame", "mdcnn_frame_crop", "mdcnn_frame_batch", "mdcnn_frame_batch_crop", "mdcnn_frame_plan", "mdcnn_frames", "mdcnn_frames_batch", "mdcnn_frames_crop", "mdcnn_frames_masked", "mdcnn_frames_plan", "mdcnn_frames_rounds", "mdcnn_input_mask", "mdcnn_read_view", "mdcnn_write_view", "mdcnn_set_option", "mdcnn_profile_read", "mdcnn_profile_read_launches", "mdcnn_bench_copy", "mdcnn_bench_mfma",
-           "mdcnn_pack_weights", "mdcnn_last_error", "mdcnn_version"]
+           "mdcnn_pack_weights", "mdcnn_group_norm_bytes", "mdcnn_group_norm", "mdcnn_group_norm_backward", "mdcnn_last_error", "mdcnn_version"]
 
 
 class mdcnn_buffer_desc(C.Structure):
@@ -49,6 +50,16 @@ class mdcnn_conv_desc(C.Structure):
 class mdcnn_mask_params(C.Structure):
     _fields_ = [("theta", C.c_float), ("sens_base", C.c_float), ("sens_gain", C.c_float), ("pool", C.c_int),
                 ("suppress", C.c_int), ("dilate", C.c_int)]
+
+
+class mdcnn_strides(C.Structure):
+    _fields_ = [("n", C.c_longlong), ("y", C.c_longlong), ("x", C.c_longlong)]
+
+
+class mdcnn_group_norm_desc(C.Structure):
+    _fields_ = [("N", C.c_int), ("H", C.c_int), ("W", C.c_int), ("C", C.c_int), ("groups", C.c_int), ("dtype", C.c_int), ("act", C.c_int),
+                ("eps", C.c_float), ("gamma_dev", C.c_void_p), ("beta_dev", C.c_void_p), ("xs", mdcnn_strides), ("ys", mdcnn_strides),
+                ("ds", mdcnn_strides)]
 
 
 class MdcnnError(RuntimeError):
@@ -103,6 +114,9 @@ def lib():
         L.mdcnn_profile_read_launches.argtypes = [C.c_int, ip, ip, ip, C.POINTER(C.c_float), ip]
         L.mdcnn_bench_copy.argtypes = [vp, vp, sz, vp]
         L.mdcnn_bench_mfma.argtypes = [C.c_int, C.c_int, vp, vp, C.POINTER(C.c_double)]
+        L.mdcnn_group_norm_bytes.argtypes = [C.POINTER(mdcnn_group_norm_desc), C.c_int, C.POINTER(sz)]
+        L.mdcnn_group_norm.argtypes = [C.POINTER(mdcnn_group_norm_desc)] + [vp] * 5 + [sz, vp]
+        L.mdcnn_group_norm_backward.argtypes = [C.POINTER(mdcnn_group_norm_desc)] + [vp] * 8 + [sz, vp]
         L.mdcnn_last_error.restype = C.c_char_p
         L.mdcnn_version.restype = C.c_char_p
         for name in EXPORTS:
@@ -379,3 +393,19 @@ def mdcnn_read_view(buf: int, what: int, dst_ptr: int, nbytes: int, stream: int 
 
 def mdcnn_write_view(buf: int, what: int, src_ptr: int, nbytes: int, stream: int = 0):
     _check(lib().mdcnn_write_view(buf, what, src_ptr, nbytes, stream))
+
+
+def mdcnn_group_norm_bytes(desc: mdcnn_group_norm_desc, backward: bool = False) -> int:
+    n = C.c_size_t()
+    _check(lib().mdcnn_group_norm_bytes(C.byref(desc), int(backward), C.byref(n)))
+    return n.value
+
+
+def mdcnn_group_norm(desc: mdcnn_group_norm_desc, x_ptr, y_ptr, mean_ptr, rstd_ptr, work_ptr, work_bytes: int, stream: int = 0):
+    _check(lib().mdcnn_group_norm(C.byref(desc), x_ptr, y_ptr, mean_ptr, rstd_ptr, work_ptr, work_bytes, stream))
+
+
+def mdcnn_group_norm_backward(desc: mdcnn_group_norm_desc, x_ptr, dy_ptr, mean_ptr, rstd_ptr, dx_ptr, dgamma_ptr, dbeta_ptr, work_ptr,
+                              work_bytes: int, stream: int = 0):
+    _check(lib().mdcnn_group_norm_backward(C.byref(desc), x_ptr, dy_ptr, mean_ptr, rstd_ptr, dx_ptr, dgamma_ptr, dbeta_ptr, work_ptr,
+                                           work_bytes, stream))

@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "mdcnn_internal.h"
+#include "ops_internal.h"
 
 using namespace mdcnn;
 
@@ -63,6 +64,10 @@ mdcnn_status fail(mdcnn_status st, const char* fmt, ...) {
     va_end(ap);
     return st;
 }
+
+}  // namespace
+mdcnn_status mdcnn::fail_with(mdcnn_status st, const char* text) { return fail(st, "%s", text); }
+namespace {
 
 size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 size_t esize(int dtype) { return dtype == MDCNN_F16 ? 2 : 4; }

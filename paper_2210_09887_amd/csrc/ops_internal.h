@@ -1,0 +1,40 @@
+// Jobs of the operators behind the feature maps, as the host fills them in and the kernels read them.
+#pragma once
+
+#include "mdcnn_internal.h"
+
+namespace mdcnn {
+
+// Sets the text of mdcnn_last_error (mdcnn_api.hip).
+mdcnn_status fail_with(mdcnn_status st, const char* text);
+
+inline size_t storage_bytes(int dtype) { return dtype == MDCNN_F32 ? 4 : 2; }
+
+// Group norm -----------------------------------------------------------------------------------------------------------
+struct NormJob {
+    const void* x;
+    const void* dy;              // gradients only
+    void* y;                     // forward: the output; gradients: dx
+    const float* gamma;          // nullptr: ones
+    const float* beta;           // nullptr: zeros
+    float* mean;                 // [N][groups], written forward, read for gradients
+    float* rstd;
+    float* dgamma;               // gradients only
+    float* dbeta;
+    float* part;                 // [N][chunks][groups][2]: mean and sum of squares about it; gradients: the two sums
+    float* joined;               // [N][groups][2] gradients, where the chunks are joined by a launch of their own
+    float* cpart;                // [N * chunks][C][2] gradients: sums of every channel
+    mdcnn_strides xs, ys, ds;    // of x; of y (or dx); of dy
+    int N, W, P, C, groups, cpg; // P = H * W pixels of an image
+    int flat;                    // the rows of all maps follow one another: pixel p lies at p * stride.x
+    int slice, slices;           // channels of a block: whole groups
+    int lanes, row_lanes;        // threads beside one another over a slice's vectors, rows of threads
+    int rows, chunks;            // pixels of a block, blocks of an image
+    int act;
+    float eps, inv_count;        // 1 / (P * cpg)
+};
+// vec: channels to a vector (1, or 16 bytes of them).  held: 16-byte vectors (or single channels) a thread keeps in registers, 0: in chunks.
+hipError_t launch_norm(const NormJob& j, int dtype, int vec, int held, hipStream_t st);
+hipError_t launch_norm_grad(const NormJob& j, int dtype, int vec, int held, hipStream_t st);
+
+}  // namespace mdcnn

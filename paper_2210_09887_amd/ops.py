@@ -1,0 +1,118 @@
+"""Operators behind the feature maps, on device tensors: group norm with an activation.
+
+Argument marshalling only: shapes, strides and types are taken from the tensors, outputs and workspaces come from torch, the
+work is enqueued on the current stream of the tensors' device.  `group_norm_act` is the same for autograd.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import binding as B
+
+_DTYPE = {torch.float32: B.MDCNN_F32, torch.float16: B.MDCNN_F16, torch.bfloat16: B.MDCNN_BF16}
+_ACT = {"none": B.MDCNN_ACT_NONE, "relu": B.MDCNN_ACT_RELU, "silu": B.MDCNN_ACT_SILU}
+
+
+def _stream(dev):
+    return torch.cuda.current_stream(dev).cuda_stream
+
+
+def _need(ok, text):
+    if not ok:
+        raise ValueError(text)
+
+
+def _on(dev, **tensors):
+    """Every given tensor is on the GPU `dev`: a pointer of another device would be read there."""
+    _need(dev.type == "cuda", "mdcnn needs GPU tensors: there is no CPU path")
+    for name, t in tensors.items():
+        _need(t is None or t.device == dev, f"{name} is on {None if t is None else t.device}, not on {dev}")
+
+
+def _floats(name, t, n):
+    _need(t is None or (t.dtype == torch.float32 and t.numel() == n and t.is_contiguous()), f"{name}: {n} contiguous float32 values")
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _work(nbytes, dev):
+    return torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+
+
+# -- group norm -----------------------------------------------------------------------------------------------------------
+def _map(name, t, like=None):
+    _need(t.dim() == 4 and (like is None or t.shape == like.shape), f"{name}: a map [N, H, W, C]" + ("" if like is None else f" of shape {tuple(like.shape)}"))
+    _need(t.dtype in _DTYPE and (like is None or t.dtype == like.dtype), f"{name}: float32, float16 or bfloat16" + ("" if like is None else ", as x"))
+    _need(t.stride(3) == 1 or t.shape[3] == 1, f"{name}: channels last")
+    return B.mdcnn_strides(t.stride(0), t.stride(1), t.stride(2))
+
+
+def _norm_desc(x, groups, gamma, beta, eps, act):
+    _need(act in _ACT, f"act: one of {', '.join(_ACT)}")
+    xs = _map("x", x)
+    N, H, W, C = x.shape
+    _on(x.device, gamma=gamma, beta=beta)
+    _floats("gamma", gamma, C)
+    _floats("beta", beta, C)
+    return B.mdcnn_group_norm_desc(N, H, W, C, int(groups), _DTYPE[x.dtype], _ACT[act], eps, _ptr(gamma), _ptr(beta), xs, xs, xs)
+
+
+def group_norm(x, groups, gamma=None, beta=None, eps=1e-5, act="none", out=None):
+    """y = act(gamma (x - mean) / sqrt(variance + eps) + beta) over every image and group of channels of x [N, H, W, C].
+
+    x may be a view with any strides as long as its channels lie side by side.  Returns (y, mean, rstd), the statistics
+    [N, groups] in float32."""
+    d = _norm_desc(x, groups, gamma, beta, eps, act)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _on(x.device, out=out)
+    d.ys = _map("out", out, x)
+    n = B.mdcnn_group_norm_bytes(d)
+    stats = torch.empty((2, x.shape[0], int(groups)), dtype=torch.float32, device=x.device)
+    work = _work(n, x.device)
+    with torch.cuda.device(x.device):
+        B.mdcnn_group_norm(d, x.data_ptr(), out.data_ptr(), stats[0].data_ptr(), stats[1].data_ptr(), _ptr(work), n, _stream(x.device))
+    return out, stats[0], stats[1]
+
+
+def group_norm_backward(x, dy, mean, rstd, groups, gamma=None, beta=None, act="none"):
+    """Gradients (dx, dgamma, dbeta) of group_norm from the gradient dy of y and the statistics it returned."""
+    d = _norm_desc(x, groups, gamma, beta, 0.0, act)
+    _on(x.device, dy=dy, mean=mean, rstd=rstd)
+    d.ds = _map("dy", dy, x)
+    _floats("mean", mean, x.shape[0] * int(groups))
+    _floats("rstd", rstd, x.shape[0] * int(groups))
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    d.ys = _map("dx", dx, x)
+    n = B.mdcnn_group_norm_bytes(d, True)
+    grads = torch.empty((2, x.shape[3]), dtype=torch.float32, device=x.device)
+    work = _work(n, x.device)
+    with torch.cuda.device(x.device):
+        B.mdcnn_group_norm_backward(d, x.data_ptr(), dy.data_ptr(), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), grads[0].data_ptr(), grads[1].data_ptr(),
+                                    _ptr(work), n, _stream(x.device))
+    return dx, grads[0], grads[1]
+
+
+class _GroupNormAct(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, groups, gamma, beta, eps, act):
+        y, mean, rstd = group_norm(x, groups, gamma, beta, eps, act)
+        ctx.save_for_backward(x, gamma, beta, mean, rstd)
+        ctx.how = groups, act
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, gamma, beta, mean, rstd = ctx.saved_tensors
+        groups, act = ctx.how
+        if dy.stride(3) != 1 and dy.shape[3] != 1:
+            dy = dy.contiguous()
+        dx, dgamma, dbeta = group_norm_backward(x, dy, mean, rstd, groups, gamma, beta, act)
+        return dx, None, None if gamma is None else dgamma, None if beta is None else dbeta, None, None
+
+
+def group_norm_act(x, groups, gamma=None, beta=None, eps=1e-5, act="none"):
+    """y of group_norm for autograd: gradients of x, gamma and beta."""
+    return _GroupNormAct.apply(x, groups, gamma, beta, eps, act)

@@ -1,0 +1,238 @@
+"""Group norm with an activation against the formula in 64 bits, its gradients against the formula's and against differences."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+EPS = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+TYPES = list(EPS)
+
+
+def act64(u, act):
+    return u * torch.sigmoid(u) if act == "silu" else u.clamp(min=0) if act == "relu" else u
+
+
+def reference(x, groups, gamma, beta, eps, act):
+    """y, mean, rstd in 64 bits on the CPU; differentiable."""
+    N, H, W, C = x.shape
+    v = x.reshape(N, H * W, groups, C // groups)
+    mean = v.mean((1, 3), keepdim=True)
+    var = ((v - mean) ** 2).mean((1, 3), keepdim=True)
+    rstd = 1 / torch.sqrt(var + eps)
+    u = ((v - mean) * rstd).reshape(N, H, W, C)
+    u = u if gamma is None else u * gamma
+    u = u if beta is None else u + beta
+    return act64(u, act), mean.reshape(N, groups), rstd.reshape(N, groups)
+
+
+def far(got, want):
+    """2-norm of the difference over that of the result."""
+    got, want = got.detach().double().cpu(), want.detach().double()
+    return float((got - want).norm() / want.norm().clamp(min=1e-300)) if want.numel() else 0.0
+
+
+# odd sizes, one pixel, one channel to a group, groups across vectors, one group of all channels, more vectors than threads
+SIZES = [(1, 1, 1, 8, 1), (2, 1, 1, 64, 32), (1, 12, 9, 256, 32), (3, 7, 5, 96, 32), (2, 37, 53, 24, 8), (1, 5, 3, 7, 7), (2, 9, 11, 33, 3), (1, 65, 63, 40, 4),
+         (1, 3, 2, 4096, 1), (1, 40, 30, 4095, 1), (2, 33, 31, 4088, 8), (1, 300, 211, 16, 16), (70, 4, 4, 32, 8), (1, 513, 700, 8, 1)]
+
+
+def inputs(N, H, W, C, dtype, seed, shift=0.0):
+    g = torch.Generator().manual_seed(seed)
+    x = (torch.randn((N, H, W, C), generator=g) * (0.3 + torch.rand(C, generator=g)) + torch.randn(C, generator=g) + shift).to(dtype)
+    gamma, beta = 1 + 0.3 * torch.randn(C, generator=g), 0.3 * torch.randn(C, generator=g)
+    dy = torch.randn((N, H, W, C), generator=g).to(dtype)
+    return x, gamma, beta, dy
+
+
+def check(x, gamma, beta, dy, groups, act, eps=1e-5):
+    from paper_2210_09887_amd import ops
+    u = EPS[x.dtype]
+    x64 = x.double().requires_grad_()
+    g64 = None if gamma is None else gamma.double().requires_grad_()
+    b64 = None if beta is None else beta.double().requires_grad_()
+    want, mean, rstd = reference(x64, groups, g64, b64, eps, act)
+    want.backward(dy.double())
+    xd, dyd = x.cuda(), dy.cuda()
+    gd, bd = (None if t is None else t.cuda() for t in (gamma, beta))
+    y, m, r = ops.group_norm(xd, groups, gd, bd, eps, act)
+    # one rounding of the result (each at most u of its value), the arithmetic of 32 bits below it: 2^-24 a step, some ten steps, a
+    # statistic over n values that are up to |mean| / deviation times larger than what is left of them
+    lift = 1 + float((mean.abs() * rstd).max())
+    tol = u + 32 * 2.0 ** -24 * lift
+    assert far(y, want) < tol, "y"
+    assert float((m.double().cpu() - mean).abs().max()) < 8 * 2.0 ** -24 * (float(mean.abs().max()) + float((1 / rstd).max())), "mean"
+    assert far(r, rstd) < 32 * 2.0 ** -24 * lift, "rstd"
+    dx, dg, db = ops.group_norm_backward(xd, dyd, m, r, groups, gd, bd, act)
+    # dx is a difference of three terms: what is left of them can be smaller than they are (one value to a group leaves nothing)
+    size = float((rstd.repeat_interleave(x.shape[3] // groups, 1)[:, None, None] * (dy.double() * (1 if g64 is None else g64.detach()))).norm())
+    off = float((dx.double().cpu() - x64.grad).norm())
+    assert off < tol * float(x64.grad.norm()) + 64 * 2.0 ** -24 * lift * size, "dx"
+    rows = dy.double().abs().sum((0, 1, 2))
+    zs = ((x64.detach() - mean.detach().repeat_interleave(x.shape[3] // groups, 1)[:, None, None]) * rstd.detach().repeat_interleave(x.shape[3] // groups, 1)[:, None, None])
+    if g64 is not None:
+        assert float(((dg.double().cpu() - g64.grad).abs() / ((dy.double() * zs).abs().sum((0, 1, 2)) + rows).clamp(min=1e-30)).max()) < 64 * 2.0 ** -24 * lift, "dgamma"
+    if b64 is not None:
+        assert float(((db.double().cpu() - b64.grad).abs() / rows.clamp(min=1e-30)).max()) < 64 * 2.0 ** -24 * lift, "dbeta"
+    return y, m, r, dx, dg, db
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("size", SIZES, ids=str)
+def test_sizes_and_types(size, dtype):
+    N, H, W, C, groups = size
+    x, gamma, beta, dy = inputs(N, H, W, C, dtype, 1)
+    check(x, gamma, beta, dy, groups, "silu")
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "silu"])
+@pytest.mark.parametrize("plain", [False, True])
+def test_activations_with_and_without_scale(act, plain):
+    x, gamma, beta, dy = inputs(2, 19, 23, 48, torch.float32, 2)
+    check(x, None if plain else gamma, None if plain else beta, dy, 6, act)
+
+
+@pytest.mark.parametrize("size", [(2, 11, 9, 32, 4), (1, 150, 130, 32, 4)], ids=str)
+def test_a_mean_far_from_zero_costs_no_digits(size):
+    N, H, W, C, groups = size
+    x, gamma, beta, dy = inputs(N, H, W, C, torch.float32, 3, shift=300.0)
+    check(x, gamma, beta, dy, groups, "silu")
+    x[0, 0, 0] = 40000.0                                 # the pixel sums start from is an outlier
+    check(x, gamma, beta, dy, groups, "silu")
+
+
+@pytest.mark.parametrize("size", [(2, 13, 17, 40, 5), (1, 160, 170, 40, 5)], ids=str)
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_views_keep_their_strides(size, dtype):
+    """Crops, slices of the channels at any element, maps with rows and columns exchanged, a gradient that is one value everywhere."""
+    from paper_2210_09887_amd import ops
+    N, H, W, C, groups = size
+    x, gamma, beta, dy = inputs(N, H + 3, W + 2, C + 8, dtype, 4)
+    xd, dyd, g, b = x.cuda(), dy.cuda(), gamma.cuda()[:C], beta.cuda()[:C]
+    for c0 in (0, 8, 3):
+        crop = xd[:, 2:2 + H, 1:1 + W, c0:c0 + C]
+        flip = xd.transpose(1, 2)[:, :W, :H, c0:c0 + C]
+        for v in (crop, flip):
+            one = dyd[:1, :1, :1, :C].expand(v.shape)
+            d = dyd[:, :v.shape[1], :v.shape[2], 1:1 + C] if v is crop else dyd.transpose(1, 2)[:, :W, :H, :C]
+            want = ops.group_norm(v.contiguous(), groups, g, b, 1e-5, "relu")
+            got = ops.group_norm(v, groups, g, b, 1e-5, "relu")
+            assert far(got[0], want[0].double().cpu()) < 2 * EPS[dtype] and far(got[1], want[1].double().cpu()) < 1e-5
+            for dd in (d, one):
+                a = ops.group_norm_backward(v, dd, *want[1:], groups, g, b, "relu")
+                w = ops.group_norm_backward(v.contiguous(), dd.contiguous(), *want[1:], groups, g, b, "relu")
+                assert all(far(p, q.double().cpu()) < 2 * EPS[dtype] + 1e-5 for p, q in zip(a, w))
+    # into a crop of a larger map: what lies around it stays
+    big = torch.full((N, H + 3, W + 2, C + 8), 7.0, dtype=dtype, device="cuda")
+    out = big[:, 2:2 + H, 1:1 + W, 8:8 + C]
+    ops.group_norm(xd[:, :H, :W, :C], groups, g, b, out=out)
+    assert torch.equal(out, ops.group_norm(xd[:, :H, :W, :C], groups, g, b, out=torch.empty_like(big)[:, 2:2 + H, 1:1 + W, 8:8 + C])[0])
+    out.fill_(7.0)
+    assert bool((big == 7.0).all())
+
+
+@pytest.mark.parametrize("size", [(2, 6, 5, 32, 4), (1, 200, 190, 32, 4)], ids=str)
+def test_in_place(size):
+    from paper_2210_09887_amd import ops
+    N, H, W, C, groups = size
+    x, gamma, beta, dy = (t.cuda() for t in inputs(N, H, W, C, torch.float16, 5))
+    want = ops.group_norm(x, groups, gamma, beta, act="silu")[0]
+    got = ops.group_norm(x, groups, gamma, beta, act="silu", out=x)[0]
+    assert got.data_ptr() == x.data_ptr() and torch.equal(got, want)
+
+
+def test_the_same_bits_twice_and_on_another_stream():
+    from paper_2210_09887_amd import ops
+    x, gamma, beta, dy = (t.cuda() for t in inputs(3, 90, 110, 96, torch.bfloat16, 6))
+    first = check(x.cpu(), gamma.cpu(), beta.cpu(), dy.cpu(), 32, "silu")
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        y, m, r = ops.group_norm(x, 32, gamma, beta, 1e-5, "silu")
+        again = (y, m, r, *ops.group_norm_backward(x, dy, m, r, 32, gamma, beta, "silu"))
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+def test_values_that_are_not_finite_stay_in_their_image_and_group():
+    from paper_2210_09887_amd import ops
+    x, gamma, beta, dy = (t.cuda() for t in inputs(3, 8, 9, 32, torch.float32, 7))
+    clean = ops.group_norm(x, 4, gamma, beta, act="silu")[0]
+    for bad in (float("inf"), float("nan")):
+        z = x.clone()
+        z[1, 3, 4, 9] = bad
+        y = ops.group_norm(z, 4, gamma, beta, act="silu")[0]
+        hit = torch.zeros_like(y, dtype=torch.bool)
+        hit[1, :, :, 8:16] = True
+        assert bool(torch.isnan(y[hit]).all()) and torch.equal(y[~hit], clean[~hit])
+
+
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_gradients_against_differences(act):
+    """(f(x + h d) - f(x - h d)) / 2 h of the kernel's own outputs in fp32, summed in 64 bits: the step's error is of order h^2,
+    that of the outputs 2^-24 sqrt(values) / h."""
+    from paper_2210_09887_amd import ops
+    x, gamma, beta, dy = inputs(2, 7, 9, 24, torch.float32, 8)
+    d = torch.randn(x.shape, generator=torch.Generator().manual_seed(9))
+    h = 2.0 ** -7
+    f = lambda t: float((ops.group_norm(t.cuda(), 3, gamma.cuda(), beta.cuda(), 1e-5, act)[0].double().cpu() * dy.double()).sum())  # noqa: E731
+    slope = (f(x + h * d) - f(x - h * d)) / (2 * h)
+    _, m, r = ops.group_norm(x.cuda(), 3, gamma.cuda(), beta.cuda(), 1e-5, act)
+    dx = ops.group_norm_backward(x.cuda(), dy.cuda(), m, r, 3, gamma.cuda(), beta.cuda(), act)[0]
+    want = float((dx.double().cpu() * d.double()).sum())
+    size = float(dx.double().cpu().norm() * d.double().norm())
+    assert abs(slope - want) < 4 * h * h * size + 2.0 ** -22 * float(dy.double().norm()) / h * 8
+
+
+def test_autograd():
+    from paper_2210_09887_amd import ops
+    x, gamma, beta, dy = (t.cuda() for t in inputs(2, 5, 6, 16, torch.float32, 10))
+    x, gamma, beta = x.requires_grad_(), gamma.requires_grad_(), beta.requires_grad_()
+    y = ops.group_norm_act(x, 4, gamma, beta, act="silu")
+    y.backward(dy)
+    _, m, r = ops.group_norm(x.detach(), 4, gamma.detach(), beta.detach(), act="silu")
+    want = ops.group_norm_backward(x.detach(), dy, m, r, 4, gamma.detach(), beta.detach(), "silu")
+    assert all(torch.equal(a, b) for a, b in zip((x.grad, gamma.grad, beta.grad), want))
+    y = ops.group_norm_act(x, 4, gamma, beta, act="silu")
+    y.sum().backward()                                   # a gradient of stride 0
+
+
+def test_no_images():
+    from paper_2210_09887_amd import ops
+    x = torch.empty((0, 4, 4, 8), device="cuda")
+    y, m, r = ops.group_norm(x, 2)
+    assert y.shape == x.shape and m.shape == (0, 2)
+    dx, dg, db = ops.group_norm_backward(x, x, m, r, 2, torch.ones(8, device="cuda"), torch.zeros(8, device="cuda"))
+    torch.cuda.synchronize()
+    assert dx.shape == x.shape and not dg.any() and not db.any()
+
+
+def test_captured_in_a_graph():
+    from paper_2210_09887_amd import ops
+    x, gamma, beta, dy = (t.cuda() for t in inputs(2, 60, 70, 64, torch.float16, 11))
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        ops.group_norm(x, 8, gamma, beta, act="silu")
+    s.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        y, m, r = ops.group_norm(x, 8, gamma, beta, act="silu")
+        dx, dg, db = ops.group_norm_backward(x, dy, m, r, 8, gamma, beta, "silu")
+    for k in range(3):
+        x.add_(0.25 * k)
+        g.replay()
+        torch.cuda.synchronize()
+        want = ops.group_norm(x, 8, gamma, beta, act="silu")
+        grads = ops.group_norm_backward(x, dy, *want[1:], 8, gamma, beta, "silu")
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((y, m, r, dx, dg, db), (*want, *grads))), k
+
+
+def test_refusals_of_tensors():
+    from paper_2210_09887_amd import ops
+    x = torch.zeros((1, 4, 4, 8), device="cuda")
+    for bad in (lambda: ops.group_norm(x.cpu(), 2), lambda: ops.group_norm(x.double(), 2), lambda: ops.group_norm(x[0], 2), lambda: ops.group_norm(x.transpose(2, 3), 2),
+                lambda: ops.group_norm(x, 2, torch.ones(7, device="cuda")), lambda: ops.group_norm(x, 2, torch.ones(8)), lambda: ops.group_norm(x, 2, act="gelu"),
+                lambda: ops.group_norm(x, 2, out=torch.zeros((1, 4, 4, 8), dtype=torch.float16, device="cuda")),
+                lambda: ops.group_norm_backward(x, x, torch.zeros(3, device="cuda"), torch.zeros(2, device="cuda"), 2)):
+        with pytest.raises(ValueError):
+            bad()

@@ -1,0 +1,57 @@
+"""Host-side checks of the operators behind the feature maps (no GPU): arguments that must be refused before anything is enqueued."""
+import ctypes as C
+
+import pytest
+
+from paper_2210_09887_amd import binding as B
+
+FAKE = 0x7F0000000000          # an aligned address that is never dereferenced on the host
+
+
+def refused(status, call, *args):
+    with pytest.raises(B.MdcnnError) as e:
+        call(*args)
+    assert e.value.status == status and B.mdcnn_last_error()
+
+
+def norm_desc(**kw):
+    N, H, W, Cc = kw.get("N", 2), kw.get("H", 6), kw.get("W", 5), kw.get("C", 16)
+    s = B.mdcnn_strides(H * W * Cc, W * Cc, Cc)
+    d = B.mdcnn_group_norm_desc(N, H, W, Cc, 4, B.MDCNN_F16, B.MDCNN_ACT_SILU, 1e-5, None, None, s, s, s)
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return d
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=3), 3), (dict(dtype=-1), 3), (dict(N=-1), 2), (dict(H=0), 2), (dict(W=0), 2), (dict(groups=0), 2), (dict(groups=3), 2), (dict(C=4100), 5),
+    (dict(H=1 << 13, W=1 << 12), 5), (dict(act=3), 2), (dict(eps=-1.0), 2), (dict(eps=float("nan")), 2), (dict(xs=B.mdcnn_strides(-1, 80, 16)), 2),
+    (dict(ys=B.mdcnn_strides(480, 80, 15)), 2), (dict(ys=B.mdcnn_strides(480, 79, 16)), 2), (dict(ys=B.mdcnn_strides(479, 80, 16)), 2), (dict(gamma_dev=FAKE + 2), 4)])
+def test_group_norm_descriptors(kw, status):
+    refused(status, B.mdcnn_group_norm_bytes, norm_desc(**kw))
+    refused(status, B.mdcnn_group_norm, norm_desc(**kw), FAKE, FAKE, FAKE, FAKE, FAKE, 1 << 30)
+
+
+def test_group_norm_arguments():
+    big = dict(H=300, W=300)                             # does not fit the registers of a block: needs a workspace
+    n = B.mdcnn_group_norm_bytes(norm_desc(**big))
+    assert n > 0 and B.mdcnn_group_norm_bytes(norm_desc()) == 0
+    call = B.mdcnn_group_norm
+    refused(5, call, norm_desc(**big), FAKE, FAKE, FAKE, FAKE, FAKE, n - 1)
+    refused(1, call, norm_desc(**big), FAKE, FAKE, FAKE, FAKE, None, n)
+    refused(4, call, norm_desc(**big), FAKE, FAKE, FAKE, FAKE, FAKE + 8, n)
+    refused(4, call, norm_desc(**big), FAKE + 1, FAKE, FAKE, FAKE, FAKE, n)
+    for k in range(4):
+        args = [FAKE] * 4
+        args[k] = None
+        refused(1, call, norm_desc(**big), *args, FAKE, n)
+    n = B.mdcnn_group_norm_bytes(norm_desc(**big), True)
+    call = B.mdcnn_group_norm_backward
+    refused(5, call, norm_desc(**big), *[FAKE] * 8, n - 1)
+    refused(2, call, norm_desc(ds=B.mdcnn_strides(0, 0, -1), **big), *[FAKE] * 8, n)
+    for k in range(7):
+        args = [FAKE] * 7
+        args[k] = None
+        refused(1, call, norm_desc(**big), *args, FAKE, n)
+    assert B.lib().mdcnn_group_norm_bytes(None, 0, C.byref(C.c_size_t())) == 1
+    assert B.lib().mdcnn_group_norm_bytes(C.byref(norm_desc()), 0, None) == 1
