@@ -643,6 +643,41 @@ mdcnn_status mdcnn_group_norm_backward(const mdcnn_group_norm_desc* d, const voi
                                        float* dgamma_dev, float* dbeta_dev, void* work_dev,
                                        size_t work_bytes, void* stream);
 
+/* Rotary positions.  The first `turned` channels of a head are turned/2 pairs; pair i of a token at position p is turned by
+ * the angle p f_i:  (a, b) -> m (a cos - b sin, a sin + b cos).  f_i is held as a step in 2^64ths of a turn, so that p times
+ * the step, modulo 2^64, is the angle without a loss at any position. */
+typedef enum {
+    MDCNN_ROTARY_PLAIN = 0,   /* f_i = base^(-i / n), n pairs to an axis                */
+    MDCNN_ROTARY_LINEAR = 1,  /* f_i / factor                                           */
+    MDCNN_ROTARY_BASE = 2,    /* base * factor^(n / (n - 1)) for base: the slowest pair is slowed by factor, the fastest kept */
+    MDCNN_ROTARY_PARTS = 3    /* pairs that turn fewer than `slow` times within `original` positions: f_i / factor; more than */
+                              /* `fast` times: f_i; in between a mix that is linear in the number of turns                    */
+} mdcnn_rotary_scaling;
+typedef struct {
+    int turned;               /* even                                                   */
+    int axes;                 /* 1..4 positions per token (row, column, frame ..); the pairs are dealt out in equal  */
+                              /* runs, turned a multiple of 2 axes                      */
+    double base;              /* > 1                                                    */
+    int scaling;              /* mdcnn_rotary_scaling                                   */
+    double factor;            /* >= 1                                                   */
+    double original, slow, fast;   /* MDCNN_ROTARY_PARTS: > 0, 0 <= slow < fast         */
+} mdcnn_rotary_desc;
+/* Host-only: steps[turned / 2] of the frequencies above (to be copied to the device once). */
+mdcnn_status mdcnn_rotary_table(const mdcnn_rotary_desc* d, uint64_t* steps);
+
+typedef struct {              /* queries or keys: heads of `dim` channels, channels side by side */
+    const void* x_dev;
+    void* y_dev;              /* may be x_dev with the same strides                     */
+    int heads;
+    long long x_token, x_head, y_token, y_head;   /* elements between tokens / heads    */
+} mdcnn_heads;
+/* One or two maps (queries and keys) of `tokens` tokens in one launch.  pos_dev: tokens x axes positions, any int32.
+ * interleaved: 0 pairs (i, i + turned/2), 1 pairs (2 i, 2 i + 1).  inverse: 1 turns back (sin negated, still times magnitude):
+ * the gradient.  Channels from `turned` to dim are copied. */
+mdcnn_status mdcnn_rotary(const mdcnn_heads* maps, int n_maps, int tokens, int dim, int dtype,
+                          const int* pos_dev, int axes, const uint64_t* steps_dev, int turned,
+                          int interleaved, int inverse, float magnitude, void* stream);
+
 const char* mdcnn_last_error(void);
 const char* mdcnn_version(void);
 

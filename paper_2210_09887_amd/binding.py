@@ -16,6 +16,7 @@ LIB_PATH = os.path.join(_HERE, "libmdcnn.so")
 MDCNN_OK = 0
 MDCNN_F32, MDCNN_F16, MDCNN_BF16 = 0, 1, 2
 MDCNN_ACT_NONE, MDCNN_ACT_RELU, MDCNN_ACT_SILU = 0, 1, 2
+MDCNN_ROTARY_PLAIN, MDCNN_ROTARY_LINEAR, MDCNN_ROTARY_BASE, MDCNN_ROTARY_PARTS = range(4)
 MDCNN_SITE_INPUT, MDCNN_SITE_PREACT, MDCNN_SITE_OUTPUT = 0, 1, 2
 (MDCNN_VIEW_A, MDCNN_VIEW_P, MDCNN_VIEW_DELTA, MDCNN_VIEW_FLAGS, MDCNN_VIEW_LIST,
  MDCNN_VIEW_CLIST, MDCNN_VIEW_STATS, MDCNN_VIEW_OUT, MDCNN_VIEW_POOL_PREV, MDCNN_VIEW_CROP_OUT,
@@ -32,7 +33,7 @@ STATUS_NAMES = {0: "OK", 1: "ERR_NULL", 2: "ERR_SHAPE", 3: "ERR_DTYPE", 4: "ERR_
 EXPORTS = ["mdcnn_conv_border", "mdcnn_conv_tiles", "mdcnn_rect_tiles", "mdcnn_gather_tile", "mdcnn_buffer_bytes", "mdcnn_create_buffer", "mdcnn_destroy_buffer",
            "mdcnn_shift_camera", "mdcnn_set_crop", "mdcnn_layer_forward", "mdcnn_layer_forward_noalloc", "mdcnn_net_create", "mdcnn_net_destroy",
            "mdcnn_frame", "mdcnn_frame_crop", "mdcnn_frame_batch", "mdcnn_frame_batch_crop", "mdcnn_frame_plan", "mdcnn_frames", "mdcnn_frames_batch", "mdcnn_frames_crop", "mdcnn_frames_masked", "mdcnn_frames_plan", "mdcnn_frames_rounds", "mdcnn_input_mask", "mdcnn_read_view", "mdcnn_write_view", "mdcnn_set_option", "mdcnn_profile_read", "mdcnn_profile_read_launches", "mdcnn_bench_copy", "mdcnn_bench_mfma",
-           "mdcnn_pack_weights", "mdcnn_group_norm_bytes", "mdcnn_group_norm", "mdcnn_group_norm_backward", "mdcnn_last_error", "mdcnn_version"]
+           "mdcnn_pack_weights", "mdcnn_group_norm_bytes", "mdcnn_group_norm", "mdcnn_group_norm_backward", "mdcnn_rotary_table", "mdcnn_rotary", "mdcnn_last_error", "mdcnn_version"]
 
 
 class mdcnn_buffer_desc(C.Structure):
@@ -60,6 +61,16 @@ class mdcnn_group_norm_desc(C.Structure):
     _fields_ = [("N", C.c_int), ("H", C.c_int), ("W", C.c_int), ("C", C.c_int), ("groups", C.c_int), ("dtype", C.c_int), ("act", C.c_int),
                 ("eps", C.c_float), ("gamma_dev", C.c_void_p), ("beta_dev", C.c_void_p), ("xs", mdcnn_strides), ("ys", mdcnn_strides),
                 ("ds", mdcnn_strides)]
+
+
+class mdcnn_rotary_desc(C.Structure):
+    _fields_ = [("turned", C.c_int), ("axes", C.c_int), ("base", C.c_double), ("scaling", C.c_int), ("factor", C.c_double), ("original", C.c_double),
+                ("slow", C.c_double), ("fast", C.c_double)]
+
+
+class mdcnn_heads(C.Structure):
+    _fields_ = [("x_dev", C.c_void_p), ("y_dev", C.c_void_p), ("heads", C.c_int), ("x_token", C.c_longlong), ("x_head", C.c_longlong),
+                ("y_token", C.c_longlong), ("y_head", C.c_longlong)]
 
 
 class MdcnnError(RuntimeError):
@@ -117,6 +128,8 @@ def lib():
         L.mdcnn_group_norm_bytes.argtypes = [C.POINTER(mdcnn_group_norm_desc), C.c_int, C.POINTER(sz)]
         L.mdcnn_group_norm.argtypes = [C.POINTER(mdcnn_group_norm_desc)] + [vp] * 5 + [sz, vp]
         L.mdcnn_group_norm_backward.argtypes = [C.POINTER(mdcnn_group_norm_desc)] + [vp] * 8 + [sz, vp]
+        L.mdcnn_rotary_table.argtypes = [C.POINTER(mdcnn_rotary_desc), C.POINTER(C.c_uint64)]
+        L.mdcnn_rotary.argtypes = [C.POINTER(mdcnn_heads), C.c_int, C.c_int, C.c_int, C.c_int, vp, C.c_int, vp, C.c_int, C.c_int, C.c_int, C.c_float, vp]
         L.mdcnn_last_error.restype = C.c_char_p
         L.mdcnn_version.restype = C.c_char_p
         for name in EXPORTS:
@@ -409,3 +422,17 @@ def mdcnn_group_norm_backward(desc: mdcnn_group_norm_desc, x_ptr, dy_ptr, mean_p
                               work_bytes: int, stream: int = 0):
     _check(lib().mdcnn_group_norm_backward(C.byref(desc), x_ptr, dy_ptr, mean_ptr, rstd_ptr, dx_ptr, dgamma_ptr, dbeta_ptr, work_ptr,
                                            work_bytes, stream))
+
+
+def mdcnn_rotary_table(desc: mdcnn_rotary_desc):
+    """The steps of turned / 2 pairs as a list of whole numbers below 2^64."""
+    out = (C.c_uint64 * max(1, desc.turned // 2))()
+    _check(lib().mdcnn_rotary_table(C.byref(desc), out))
+    return list(out)
+
+
+def mdcnn_rotary(maps, tokens: int, dim: int, dtype: int, pos_ptr, axes: int, steps_ptr, turned: int, interleaved: bool = False, inverse: bool = False,
+                 magnitude: float = 1.0, stream: int = 0):
+    """maps: one or two mdcnn_heads."""
+    _check(lib().mdcnn_rotary((mdcnn_heads * len(maps))(*maps), len(maps), tokens, dim, dtype, pos_ptr, axes, steps_ptr, turned, interleaved, inverse,
+                              magnitude, stream))

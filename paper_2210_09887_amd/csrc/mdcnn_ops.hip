@@ -1,9 +1,9 @@
 // Host side of the operators behind the feature maps: argument checks, launch shapes.  Allocates nothing and never waits.
-#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 
 #include <algorithm>
+#include <cmath>
 #include <numeric>
 
 #include "ops_internal.h"
@@ -152,6 +152,23 @@ mdcnn_status run_norm(const mdcnn_group_norm_desc& d, bool backward, const void*
     return launched(launch_norm(j, d.dtype, vec, held, (hipStream_t)stream), "group_norm");
 }
 
+// ---- rotary positions -----------------------------------------------------------------------------------------------------
+mdcnn_status check_heads(const mdcnn_heads& m, const char* call, const char* what, int dim, long long tokens, size_t e, bool reads, bool writes) {
+    const long long top = 1ll << 46;
+    if (m.heads < 1 || m.heads > 65535) return fail(MDCNN_ERR_SHAPE, "%s: heads of %s out of range", call, what);
+    if ((reads && !m.x_dev) || (writes && !m.y_dev)) return fail(MDCNN_ERR_NULL, "%s: %s is NULL", call, what);
+    if ((reads && !aligned(m.x_dev, e)) || (writes && !aligned(m.y_dev, e))) return fail(MDCNN_ERR_ALIGN, "%s: %s is misaligned", call, what);
+    if (reads && (m.x_token < 0 || m.x_head < 0 || m.x_token > top || m.x_head > top)) return fail(MDCNN_ERR_SHAPE, "%s: strides of %s out of range", call, what);
+    if (writes) {
+        // heads within tokens or tokens within heads: either way none may reach into the next
+        const bool within = m.heads == 1 || m.y_head >= dim;
+        if (m.y_token < dim || !within || m.y_token > top || m.y_head > top) return fail(MDCNN_ERR_SHAPE, "%s: heads of %s overlap", call, what);
+        if (m.heads > 1 && m.y_token >= m.y_head && m.y_token < (m.heads - 1) * m.y_head + dim) return fail(MDCNN_ERR_SHAPE, "%s: tokens of %s overlap", call, what);
+        if (m.heads > 1 && m.y_token < m.y_head && m.y_head < (tokens - 1) * m.y_token + dim) return fail(MDCNN_ERR_SHAPE, "%s: heads of %s overlap", call, what);
+    }
+    return MDCNN_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -178,6 +195,78 @@ mdcnn_status mdcnn_group_norm_backward(const mdcnn_group_norm_desc* d, const voi
     if (st) return st;
     if (!dgamma_dev || !dbeta_dev || (d->N && (!x_dev || !dy_dev || !mean_dev || !rstd_dev || !dx_dev))) return fail(MDCNN_ERR_NULL, "group_norm_backward: NULL argument");
     return run_norm(*d, true, x_dev, dy_dev, dx_dev, const_cast<float*>(mean_dev), const_cast<float*>(rstd_dev), dgamma_dev, dbeta_dev, work_dev, work_bytes, stream);
+}
+
+mdcnn_status mdcnn_rotary_table(const mdcnn_rotary_desc* d, uint64_t* steps) {
+    if (!d || !steps) return fail(MDCNN_ERR_NULL, "rotary_table: NULL argument");
+    if (d->axes < 1 || d->axes > 4 || d->turned < 2 || d->turned > 4096 || d->turned % (2 * d->axes)) return fail(MDCNN_ERR_SHAPE, "rotary_table: %d channels on %d axes", d->turned, d->axes);
+    if (!(d->base > 1.0) || !std::isfinite(d->base)) return fail(MDCNN_ERR_SHAPE, "rotary_table: base must be above 1");
+    if (d->scaling < MDCNN_ROTARY_PLAIN || d->scaling > MDCNN_ROTARY_PARTS) return fail(MDCNN_ERR_SHAPE, "rotary_table: unknown scaling %d", d->scaling);
+    if (d->scaling != MDCNN_ROTARY_PLAIN && (!(d->factor >= 1.0) || !std::isfinite(d->factor))) return fail(MDCNN_ERR_SHAPE, "rotary_table: factor must be 1 or more");
+    if (d->scaling == MDCNN_ROTARY_PARTS && (!(d->original > 0.0) || !(d->slow >= 0.0) || !(d->fast > d->slow) || !std::isfinite(d->original) || !std::isfinite(d->fast)))
+        return fail(MDCNN_ERR_SHAPE, "rotary_table: original > 0 and 0 <= slow < fast are needed");
+    const int n = d->turned / 2 / d->axes;
+    const double two_pi = 6.283185307179586476925;
+    double base = d->base;
+    if (d->scaling == MDCNN_ROTARY_BASE && n > 1) base *= std::pow(d->factor, (double)n / (n - 1));
+    for (int i = 0; i < d->turned / 2; ++i) {
+        double f = std::pow(base, -(double)(i % n) / n);
+        if (d->scaling == MDCNN_ROTARY_LINEAR) f /= d->factor;
+        if (d->scaling == MDCNN_ROTARY_PARTS) {
+            const double keep = std::min(1.0, std::max(0.0, (d->original * f / two_pi - d->slow) / (d->fast - d->slow)));
+            f = f * keep + f / d->factor * (1.0 - keep);
+        }
+        steps[i] = (uint64_t)std::rint(std::ldexp(f / two_pi, 64));
+    }
+    return MDCNN_OK;
+}
+
+mdcnn_status mdcnn_rotary(const mdcnn_heads* maps, int n_maps, int tokens, int dim, int dtype, const int* pos_dev, int axes, const uint64_t* steps_dev, int turned, int interleaved,
+                          int inverse, float magnitude, void* stream) {
+    if (!maps) return fail(MDCNN_ERR_NULL, "rotary: maps is NULL");
+    if (!known_dtype(dtype)) return fail(MDCNN_ERR_DTYPE, "rotary: unknown dtype %d", dtype);
+    if (n_maps < 1 || n_maps > 2) return fail(MDCNN_ERR_SHAPE, "rotary: one or two maps");
+    if (tokens < 0) return fail(MDCNN_ERR_SHAPE, "rotary: %d tokens", tokens);
+    if (dim < 2 || dim > 256) return fail(MDCNN_ERR_SIZE, "rotary: 2 to 256 channels to a head");
+    if (axes < 1 || axes > 4 || turned < 2 || turned > dim || turned % (2 * axes)) return fail(MDCNN_ERR_SHAPE, "rotary: %d of %d channels on %d axes", turned, dim, axes);
+    if ((interleaved | inverse) & ~1) return fail(MDCNN_ERR_SHAPE, "rotary: interleaved and inverse are 0 or 1");
+    if (!std::isfinite(magnitude)) return fail(MDCNN_ERR_SHAPE, "rotary: magnitude is not finite");
+    const size_t e = storage_bytes(dtype);
+    RotaryJob j{};
+    for (int i = 0; i < n_maps; ++i) {
+        mdcnn_status st = tokens ? check_heads(maps[i], "rotary", i ? "the second map" : "the first map", dim, tokens, e, true, true) : MDCNN_OK;
+        if (st) return st;
+        j.maps[i] = RotaryMap{maps[i].x_dev, maps[i].y_dev, maps[i].heads, maps[i].x_token, maps[i].x_head, maps[i].y_token, maps[i].y_head};
+    }
+    if (!tokens) return MDCNN_OK;
+    if (!pos_dev || !steps_dev) return fail(MDCNN_ERR_NULL, "rotary: positions or steps are NULL");
+    if (!aligned(pos_dev, 4) || !aligned(steps_dev, 8)) return fail(MDCNN_ERR_ALIGN, "rotary: positions or steps are misaligned");
+    // The widest vectors that the turned and the copied channels consist of and every head begins on.
+    int vec = 1;
+    for (int v : {(int)(16 / e), 4}) {
+        const size_t bytes = v * e;
+        bool ok = (interleaved ? turned : turned / 2) % v == 0 && (dim - turned) % v == 0;
+        for (int i = 0; i < n_maps; ++i) {
+            const RotaryMap& m = j.maps[i];
+            ok = ok && aligned(m.x, bytes) && aligned(m.y, bytes) && m.x_token % v == 0 && m.y_token % v == 0 && (m.heads == 1 || (m.x_head % v == 0 && m.y_head % v == 0));
+        }
+        if (ok) { vec = v; break; }
+    }
+    bool in_place = true;
+    for (int i = 0; i < n_maps; ++i) in_place = in_place && j.maps[i].x == j.maps[i].y && j.maps[i].x_token == j.maps[i].y_token && j.maps[i].x_head == j.maps[i].y_head;
+    j.pos = pos_dev; j.steps = (const unsigned long long*)steps_dev;
+    j.tokens = tokens; j.axes = axes; j.per = turned / 2 / axes; j.turned = turned;
+    j.turned_units = interleaved ? (vec > 1 ? turned / vec : turned / 2) : turned / 2 / vec;
+    j.units = j.turned_units + (in_place ? 0 : (dim - turned) / vec);
+    j.tokens_per_block = 256 / j.units;
+    j.inverse = inverse; j.magnitude = magnitude;
+    // A thread goes through up to 16 heads with the same sines; fewer where that leaves less than eight blocks to a compute unit.
+    const int heads = j.maps[0].heads + j.maps[1].heads;
+    const long long blocks = (tokens + j.tokens_per_block - 1) / j.tokens_per_block;
+    j.group = std::min(heads, 16);
+    while (j.group > 1 && blocks * ((heads + j.group - 1) / j.group) < 2048) j.group = (j.group + 1) / 2;
+    if (j.group == 1 && heads > 65535) j.group = 2;                        // (the grid's second extent)
+    return launched(launch_rotary(j, dtype, vec, interleaved != 0, (hipStream_t)stream), "rotary");
 }
 
 }  // extern "C"

@@ -37,4 +37,25 @@ struct NormJob {
 hipError_t launch_norm(const NormJob& j, int dtype, int vec, int held, hipStream_t st);
 hipError_t launch_norm_grad(const NormJob& j, int dtype, int vec, int held, hipStream_t st);
 
+// Rotary positions -------------------------------------------------------------------------------------------------------
+struct RotaryMap {
+    const void* x;
+    void* y;
+    int heads;
+    long long x_token, x_head, y_token, y_head;
+};
+struct RotaryJob {
+    RotaryMap maps[2];           // of the second, 0 heads if there is none
+    const int* pos;              // [tokens][axes]
+    const unsigned long long* steps;
+    long long tokens;
+    int axes, per;               // per: pairs to an axis
+    int turned;
+    int turned_units, units;     // vectors of a head that a thread each turns; these and those that are copied
+    int tokens_per_block, group; // group: heads a thread goes through
+    int inverse;
+    float magnitude;
+};
+hipError_t launch_rotary(const RotaryJob& j, int dtype, int vec, bool interleaved, hipStream_t st);
+
 }  // namespace mdcnn

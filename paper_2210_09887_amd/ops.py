@@ -1,4 +1,4 @@
-"""Operators behind the feature maps, on device tensors: group norm with an activation.
+"""Operators behind the feature maps, on device tensors: group norm with an activation, rotary positions.
 
 Argument marshalling only: shapes, strides and types are taken from the tensors, outputs and workspaces come from torch, the
 work is enqueued on the current stream of the tensors' device.  `group_norm_act` is the same for autograd.
@@ -116,3 +116,69 @@ class _GroupNormAct(torch.autograd.Function):
 def group_norm_act(x, groups, gamma=None, beta=None, eps=1e-5, act="none"):
     """y of group_norm for autograd: gradients of x, gamma and beta."""
     return _GroupNormAct.apply(x, groups, gamma, beta, eps, act)
+
+
+# -- rotary positions -------------------------------------------------------------------------------------------------------
+_SCALING = {"none": B.MDCNN_ROTARY_PLAIN, "linear": B.MDCNN_ROTARY_LINEAR, "base": B.MDCNN_ROTARY_BASE, "parts": B.MDCNN_ROTARY_PARTS}
+
+
+def rotary_steps(turned, axes=1, base=10000.0, scaling="none", factor=1.0, original=4096, slow=1.0, fast=32.0, device="cuda:0"):
+    """The frequencies of `turned` channels on `axes` positions as `rotary` takes them: an int64 tensor of turned / 2 steps in
+    2^64ths of a turn (the upper half of the range as negative numbers).
+
+    scaling: "none"; "linear" all turns slowed by factor; "base" the base raised so that the slowest pair is slowed by factor;
+    "parts" pairs that turn fewer than `slow` times within `original` positions slowed by factor, more than `fast` times not at all."""
+    _need(scaling in _SCALING, f"scaling: one of {', '.join(_SCALING)}")
+    steps = B.mdcnn_rotary_table(B.mdcnn_rotary_desc(int(turned), int(axes), base, _SCALING[scaling], factor, original, slow, fast))
+    return torch.tensor([n - (1 << 64) if n >= 1 << 63 else n for n in steps], dtype=torch.int64, device=device)
+
+
+def _heads(name, t, dtype, dim, tokens):
+    _need(t.dim() == 3 and t.shape[0] == tokens and t.shape[2] == dim, f"{name}: [{tokens}, heads, {dim}]")
+    _need(t.dtype == dtype, f"{name}: {dtype}")
+    _need(t.stride(2) == 1 or dim == 1, f"{name}: channels side by side")
+
+
+def rotary(maps, positions, steps, axes=1, interleaved=False, magnitude=1.0, inverse=False, out=None):
+    """Turns the first 2 * len(steps) channels of every head of one or two maps [tokens, heads, dim] (queries and keys; any strides, channels side by
+    side) by positions [tokens] or [tokens, axes] int32; the others are copied.  Returns new tensors, or `out` (which may be `maps`
+    themselves).  inverse=True turns back by the same angles, times magnitude: the gradient."""
+    first = maps[0]
+    tokens, dim, dev = first.shape[0], first.shape[-1], first.device
+    _need(1 <= len(maps) <= 2, "maps: one or two")
+    _need(first.dtype in _DTYPE, "maps: float32, float16 or bfloat16")
+    _need(positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == tokens * axes, f"positions: {tokens} x {axes} contiguous int32 values")
+    _need(steps.dtype == torch.int64 and steps.dim() == 1 and steps.is_contiguous(), "steps: contiguous int64 values of rotary_steps")
+    if out is None:
+        out = [torch.empty(m.shape, dtype=m.dtype, device=dev) for m in maps]
+    _on(dev, positions=positions, steps=steps, **{f"maps[{i}]": m for i, m in enumerate(maps)}, **{f"out[{i}]": m for i, m in enumerate(out)})
+    _need(len(out) == len(maps), "out: one tensor for each map")
+    hs = []
+    for i, (x, y) in enumerate(zip(maps, out)):
+        _heads(f"maps[{i}]", x, first.dtype, dim, tokens)
+        _heads(f"out[{i}]", y, first.dtype, dim, tokens)
+        _need(x.shape[1] == y.shape[1], "out: as many heads as maps")
+        hs.append(B.mdcnn_heads(x.data_ptr(), y.data_ptr(), x.shape[1], x.stride(0), x.stride(1), y.stride(0), y.stride(1)))
+    with torch.cuda.device(dev):
+        B.mdcnn_rotary(hs, tokens, dim, _DTYPE[first.dtype], positions.data_ptr(), axes, steps.data_ptr(), 2 * steps.numel(), interleaved, inverse, magnitude, _stream(dev))
+    return list(out)
+
+
+class _Rotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, positions, steps, axes, interleaved, magnitude, *maps):
+        ctx.save_for_backward(positions, steps)
+        ctx.how = axes, interleaved, magnitude
+        return tuple(rotary(maps, positions, steps, axes, interleaved, magnitude))
+
+    @staticmethod
+    def backward(ctx, *grads):
+        positions, steps = ctx.saved_tensors
+        axes, interleaved, magnitude = ctx.how
+        grads = [g if g.stride(2) == 1 else g.contiguous() for g in grads]
+        return (None, None, None, None, None, *rotary(grads, positions, steps, axes, interleaved, magnitude, inverse=True))
+
+
+def rotary_turn(maps, positions, steps, axes=1, interleaved=False, magnitude=1.0):
+    """`rotary` for autograd: gradients of the maps."""
+    return list(_Rotary.apply(positions, steps, axes, interleaved, magnitude, *maps))

@@ -55,3 +55,46 @@ def test_group_norm_arguments():
         refused(1, call, norm_desc(**big), *args, FAKE, n)
     assert B.lib().mdcnn_group_norm_bytes(None, 0, C.byref(C.c_size_t())) == 1
     assert B.lib().mdcnn_group_norm_bytes(C.byref(norm_desc()), 0, None) == 1
+
+
+def rotary_desc(**kw):
+    d = B.mdcnn_rotary_desc(32, 2, 10000.0, B.MDCNN_ROTARY_PARTS, 4.0, 4096.0, 1.0, 32.0)
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return d
+
+
+@pytest.mark.parametrize("kw", [dict(turned=0), dict(turned=30), dict(turned=33), dict(axes=0), dict(axes=5), dict(base=1.0), dict(base=float("nan")), dict(base=float("inf")),
+                                dict(scaling=4), dict(factor=0.5), dict(factor=float("inf")), dict(original=0.0), dict(slow=-1.0), dict(fast=1.0)])
+def test_rotary_tables(kw):
+    refused(2, B.mdcnn_rotary_table, rotary_desc(**kw))
+
+
+def test_rotary_table_values():
+    import math
+    steps = B.mdcnn_rotary_table(rotary_desc(scaling=B.MDCNN_ROTARY_PLAIN))
+    assert len(steps) == 16 and steps[:8] == steps[8:]
+    for i, s in enumerate(steps[:8]):
+        assert abs(s / 2.0 ** 64 * 2 * math.pi / 10000.0 ** (-i / 8) - 1) < 1e-14
+    slow = B.mdcnn_rotary_table(rotary_desc(scaling=B.MDCNN_ROTARY_BASE))
+    assert slow[0] == steps[0] and abs(steps[7] / slow[7] - 4) < 1e-12
+    assert B.mdcnn_rotary_table(rotary_desc(scaling=B.MDCNN_ROTARY_BASE, turned=2, axes=1)) == steps[:1]
+
+
+def heads(**kw):
+    m = B.mdcnn_heads(FAKE, FAKE, 4, 128, 32, 128, 32)
+    for k, v in kw.items():
+        setattr(m, k, v)
+    return m
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=5), 3), (dict(tokens=-1), 2), (dict(dim=1), 5), (dict(dim=257), 5), (dict(turned=34), 2), (dict(turned=0), 2), (dict(turned=30, axes=2), 2), (dict(axes=0), 2),
+    (dict(axes=5), 2), (dict(interleaved=2), 2), (dict(inverse=-1), 2), (dict(magnitude=float("nan")), 2), (dict(pos_ptr=None), 1), (dict(steps_ptr=None), 1),
+    (dict(pos_ptr=FAKE + 2), 4), (dict(steps_ptr=FAKE + 4), 4), (dict(maps=[]), 2), (dict(maps=[heads()] * 3), 2), (dict(maps=[heads(heads=0)]), 2), (dict(maps=[heads(x_dev=None)]), 1),
+    (dict(maps=[heads(y_dev=None)]), 1), (dict(maps=[heads(x_dev=FAKE + 1)]), 4), (dict(maps=[heads(x_token=-1)]), 2), (dict(maps=[heads(y_token=127)]), 2),
+    (dict(maps=[heads(y_head=31)]), 2), (dict(maps=[heads(y_token=32, y_head=95)]), 2), (dict(maps=[heads(), heads(y_token=31)]), 2)])
+def test_rotary_arguments(change, status):
+    kw = dict(maps=[heads()], tokens=3, dim=32, dtype=0, pos_ptr=FAKE, axes=1, steps_ptr=FAKE, turned=32)
+    kw.update(change)
+    refused(status, lambda: B.mdcnn_rotary(**kw))
