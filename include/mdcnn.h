@@ -678,6 +678,39 @@ mdcnn_status mdcnn_rotary(const mdcnn_heads* maps, int n_maps, int tokens, int d
                           const int* pos_dev, int axes, const uint64_t* steps_dev, int turned,
                           int interleaved, int inverse, float magnitude, void* stream);
 
+/* A cache of keys and values in pages of MDCNN_PAGE_TOKENS tokens, 8 bits a value: code * scale, one scale for each page and
+ * head.  Keys of a page lie [head][token][pitch], its values [head][pitch][token], pitch = mdcnn_cache_pitch(dim); channels
+ * from dim on are never read.  Which page holds which tokens of which sequence says a table of page numbers, n_seq rows of
+ * max_pages: tokens 64 i .. 64 i + 63 of a sequence lie in the page of entry i of its row.  Sequences may share pages that none of them writes. */
+#define MDCNN_PAGE_TOKENS 64
+typedef struct {
+    int pages, heads, dim;    /* 1 <= heads, 8 <= dim <= 256, a multiple of 8           */
+    int8_t* k_dev;            /* pages * heads * 64 * pitch bytes each, 16-byte aligned */
+    int8_t* v_dev;
+    float* k_scale_dev;       /* pages * heads                                          */
+    float* v_scale_dev;
+    const int* table_dev;     /* n_seq * max_pages page numbers; entries outside 0 .. pages - 1 hold no page */
+    int n_seq, max_pages;
+} mdcnn_cache_desc;
+/* Host-only: channels a row of `dim` takes in a page: the next of 32, 64, 96, 128, 192, 256 (0: dim out of range). */
+int mdcnn_cache_pitch(int dim);
+/* Keys and values of new tokens into their pages.  The new tokens of all sequences lie one sequence behind the other:
+ * sequence s has tokens starts_dev[s] .. starts_dev[s + 1] - 1 of the two maps (of which x_dev, heads = the cache's, and the x strides count),
+ * and they follow the held_dev[s] tokens that it has in the cache already.  A page that gets its first token takes as scale
+ * max |x| / 127 over the new tokens; one that holds some keeps its scale as long as it is large enough, else takes the larger of
+ * max |x| / 127 and 1.25 times the old one and its codes are rounded again.  Codes are rounded to nearest even.  A page and head
+ * that gets a value that is not finite has NaN for a scale until its first token is stored again.  max_new: no sequence has more new tokens.
+ * tokens: rows of the two maps; nothing beyond is touched whatever starts say.  Tokens whose table entry holds no page, or that lie beyond
+ * max_pages or max_new, are left out. */
+mdcnn_status mdcnn_cache_store(const mdcnn_cache_desc* c, const mdcnn_heads* k, const mdcnn_heads* v, int tokens,
+                               const int* starts_dev, const int* held_dev, int max_new, int dtype,
+                               void* stream);
+/* The values back: sequence s gives tokens first_dev[s] .. first_dev[s] + n - 1, n = starts_dev[s + 1] - starts_dev[s], to
+ * tokens starts_dev[s] .. of the two maps (y_dev and the y strides count).  Tokens without a page are zeros. */
+mdcnn_status mdcnn_cache_read(const mdcnn_cache_desc* c, const mdcnn_heads* k, const mdcnn_heads* v, int tokens,
+                              const int* starts_dev, const int* first_dev, int max_new, int dtype,
+                              void* stream);
+
 const char* mdcnn_last_error(void);
 const char* mdcnn_version(void);
 

@@ -17,6 +17,7 @@ MDCNN_OK = 0
 MDCNN_F32, MDCNN_F16, MDCNN_BF16 = 0, 1, 2
 MDCNN_ACT_NONE, MDCNN_ACT_RELU, MDCNN_ACT_SILU = 0, 1, 2
 MDCNN_ROTARY_PLAIN, MDCNN_ROTARY_LINEAR, MDCNN_ROTARY_BASE, MDCNN_ROTARY_PARTS = range(4)
+MDCNN_PAGE_TOKENS = 64
 MDCNN_SITE_INPUT, MDCNN_SITE_PREACT, MDCNN_SITE_OUTPUT = 0, 1, 2
 (MDCNN_VIEW_A, MDCNN_VIEW_P, MDCNN_VIEW_DELTA, MDCNN_VIEW_FLAGS, MDCNN_VIEW_LIST,
  MDCNN_VIEW_CLIST, MDCNN_VIEW_STATS, MDCNN_VIEW_OUT, MDCNN_VIEW_POOL_PREV, MDCNN_VIEW_CROP_OUT,
@@ -33,7 +34,8 @@ STATUS_NAMES = {0: "OK", 1: "ERR_NULL", 2: "ERR_SHAPE", 3: "ERR_DTYPE", 4: "ERR_
 EXPORTS = ["mdcnn_conv_border", "mdcnn_conv_tiles", "mdcnn_rect_tiles", "mdcnn_gather_tile", "mdcnn_buffer_bytes", "mdcnn_create_buffer", "mdcnn_destroy_buffer",
            "mdcnn_shift_camera", "mdcnn_set_crop", "mdcnn_layer_forward", "mdcnn_layer_forward_noalloc", "mdcnn_net_create", "mdcnn_net_destroy",
            "mdcnn_frame", "mdcnn_frame_crop", "mdcnn_frame_batch", "mdcnn_frame_batch_crop", "mdcnn_frame_plan", "mdcnn_frames", "mdcnn_frames_batch", "mdcnn_frames_crop", "mdcnn_frames_masked", "mdcnn_frames_plan", "mdcnn_frames_rounds", "mdcnn_input_mask", "mdcnn_read_view", "mdcnn_write_view", "mdcnn_set_option", "mdcnn_profile_read", "mdcnn_profile_read_launches", "mdcnn_bench_copy", "mdcnn_bench_mfma",
-           "mdcnn_pack_weights", "mdcnn_group_norm_bytes", "mdcnn_group_norm", "mdcnn_group_norm_backward", "mdcnn_rotary_table", "mdcnn_rotary", "mdcnn_last_error", "mdcnn_version"]
+           "mdcnn_pack_weights", "mdcnn_group_norm_bytes", "mdcnn_group_norm", "mdcnn_group_norm_backward", "mdcnn_rotary_table", "mdcnn_rotary", "mdcnn_cache_pitch",
+           "mdcnn_cache_store", "mdcnn_cache_read", "mdcnn_last_error", "mdcnn_version"]
 
 
 class mdcnn_buffer_desc(C.Structure):
@@ -71,6 +73,11 @@ class mdcnn_rotary_desc(C.Structure):
 class mdcnn_heads(C.Structure):
     _fields_ = [("x_dev", C.c_void_p), ("y_dev", C.c_void_p), ("heads", C.c_int), ("x_token", C.c_longlong), ("x_head", C.c_longlong),
                 ("y_token", C.c_longlong), ("y_head", C.c_longlong)]
+
+
+class mdcnn_cache_desc(C.Structure):
+    _fields_ = [("pages", C.c_int), ("heads", C.c_int), ("dim", C.c_int), ("k_dev", C.c_void_p), ("v_dev", C.c_void_p), ("k_scale_dev", C.c_void_p),
+                ("v_scale_dev", C.c_void_p), ("table_dev", C.c_void_p), ("n_seq", C.c_int), ("max_pages", C.c_int)]
 
 
 class MdcnnError(RuntimeError):
@@ -130,6 +137,10 @@ def lib():
         L.mdcnn_group_norm_backward.argtypes = [C.POINTER(mdcnn_group_norm_desc)] + [vp] * 8 + [sz, vp]
         L.mdcnn_rotary_table.argtypes = [C.POINTER(mdcnn_rotary_desc), C.POINTER(C.c_uint64)]
         L.mdcnn_rotary.argtypes = [C.POINTER(mdcnn_heads), C.c_int, C.c_int, C.c_int, C.c_int, vp, C.c_int, vp, C.c_int, C.c_int, C.c_int, C.c_float, vp]
+        L.mdcnn_cache_pitch.argtypes = [C.c_int]
+        hs, cd = C.POINTER(mdcnn_heads), C.POINTER(mdcnn_cache_desc)
+        L.mdcnn_cache_store.argtypes = [cd, hs, hs, C.c_int, vp, vp, C.c_int, C.c_int, vp]
+        L.mdcnn_cache_read.argtypes = [cd, hs, hs, C.c_int, vp, vp, C.c_int, C.c_int, vp]
         L.mdcnn_last_error.restype = C.c_char_p
         L.mdcnn_version.restype = C.c_char_p
         for name in EXPORTS:
@@ -436,3 +447,15 @@ def mdcnn_rotary(maps, tokens: int, dim: int, dtype: int, pos_ptr, axes: int, st
     """maps: one or two mdcnn_heads."""
     _check(lib().mdcnn_rotary((mdcnn_heads * len(maps))(*maps), len(maps), tokens, dim, dtype, pos_ptr, axes, steps_ptr, turned, interleaved, inverse,
                               magnitude, stream))
+
+
+def mdcnn_cache_pitch(dim: int) -> int:
+    return lib().mdcnn_cache_pitch(int(dim))
+
+
+def mdcnn_cache_store(cache: mdcnn_cache_desc, k: mdcnn_heads, v: mdcnn_heads, tokens: int, starts_ptr, held_ptr, max_new: int, dtype: int, stream: int = 0):
+    _check(lib().mdcnn_cache_store(C.byref(cache), C.byref(k), C.byref(v), tokens, starts_ptr, held_ptr, max_new, dtype, stream))
+
+
+def mdcnn_cache_read(cache: mdcnn_cache_desc, k: mdcnn_heads, v: mdcnn_heads, tokens: int, starts_ptr, first_ptr, max_new: int, dtype: int, stream: int = 0):
+    _check(lib().mdcnn_cache_read(C.byref(cache), C.byref(k), C.byref(v), tokens, starts_ptr, first_ptr, max_new, dtype, stream))

@@ -169,6 +169,51 @@ mdcnn_status check_heads(const mdcnn_heads& m, const char* call, const char* wha
     return MDCNN_OK;
 }
 
+// ---- the cache ------------------------------------------------------------------------------------------------------------
+mdcnn_status check_cache(const mdcnn_cache_desc* c, const char* call) {
+    if (!c) return fail(MDCNN_ERR_NULL, "%s: cache is NULL", call);
+    if (!mdcnn_cache_pitch(c->dim)) return fail(MDCNN_ERR_SHAPE, "%s: %d channels to a head (8 to 256, a multiple of 8)", call, c->dim);
+    if (c->heads < 1 || c->heads > 32767) return fail(MDCNN_ERR_SHAPE, "%s: %d heads", call, c->heads);
+    if (c->pages < 0 || c->n_seq < 0 || c->max_pages < 0 || c->max_pages > (1 << 24)) return fail(MDCNN_ERR_SIZE, "%s: pages, sequences or table out of range", call);
+    if (c->n_seq && (!c->k_dev || !c->v_dev || !c->k_scale_dev || !c->v_scale_dev || !c->table_dev)) return fail(MDCNN_ERR_NULL, "%s: NULL pointer in the cache", call);
+    if (!aligned(c->k_dev, 16) || !aligned(c->v_dev, 16) || !aligned(c->k_scale_dev, 4) || !aligned(c->v_scale_dev, 4) || !aligned(c->table_dev, 4))
+        return fail(MDCNN_ERR_ALIGN, "%s: misaligned pointer in the cache", call);
+    return MDCNN_OK;
+}
+
+mdcnn_status run_cache(const mdcnn_cache_desc* c, const mdcnn_heads* k, const mdcnn_heads* v, int tokens, const int* starts, const int* first, int max_new, int dtype, bool store, void* stream) {
+    const char* call = store ? "cache_store" : "cache_read";
+    mdcnn_status st = check_cache(c, call);
+    if (st) return st;
+    if (!known_dtype(dtype)) return fail(MDCNN_ERR_DTYPE, "%s: unknown dtype %d", call, dtype);
+    if (!k || !v) return fail(MDCNN_ERR_NULL, "%s: NULL map", call);
+    if (max_new < 0 || tokens < 0) return fail(MDCNN_ERR_SHAPE, "%s: max_new %d, %d tokens", call, max_new, tokens);
+    max_new = std::min(max_new, tokens);
+    if (!c->n_seq || !max_new) return MDCNN_OK;
+    if (!starts || !first) return fail(MDCNN_ERR_NULL, "%s: starts or positions are NULL", call);
+    if (!aligned(starts, 4) || !aligned(first, 4)) return fail(MDCNN_ERR_ALIGN, "%s: starts or positions are misaligned", call);
+    const size_t e = storage_bytes(dtype);
+    CacheJob j{};
+    int vec = (int)(16 / e);
+    for (const mdcnn_heads* m : {k, v}) {
+        const char* what = m == k ? "the keys" : "the values";
+        if (m->heads != c->heads) return fail(MDCNN_ERR_SHAPE, "%s: %d heads in %s, %d in the cache", call, m->heads, what, c->heads);
+        st = check_heads(*m, call, what, c->dim, tokens, e, store, !store);
+        if (st) return st;
+        const void* at = store ? m->x_dev : m->y_dev;
+        const long long token = store ? m->x_token : m->y_token, head = store ? m->x_head : m->y_head;
+        if (!aligned(at, 16) || token % vec || (m->heads > 1 && head % vec)) vec = 1;
+        (m == k ? j.k : j.v) = CacheMap{m->x_dev, m->y_dev, m->x_token, m->x_head, m->y_token, m->y_head};
+    }
+    j.k_codes = c->k_dev; j.v_codes = c->v_dev; j.k_scale = c->k_scale_dev; j.v_scale = c->v_scale_dev;
+    j.table = c->table_dev; j.starts = starts; j.first = first;
+    j.pages = c->pages; j.heads = c->heads; j.dim = c->dim; j.pitch = mdcnn_cache_pitch(c->dim);
+    j.n_seq = c->n_seq; j.max_pages = c->max_pages; j.max_new = max_new; j.tokens = tokens;
+    j.slots = (int)(((long long)max_new + MDCNN_PAGE_TOKENS - 2) / MDCNN_PAGE_TOKENS) + 1;      // the first page may be begun
+    if ((long long)j.n_seq * j.slots > 0x7fffffffll) return fail(MDCNN_ERR_SIZE, "%s: %d sequences of up to %d tokens", call, j.n_seq, max_new);
+    return launched(launch_cache(j, dtype, vec, store, (hipStream_t)stream), call);
+}
+
 }  // namespace
 
 extern "C" {
@@ -267,6 +312,21 @@ mdcnn_status mdcnn_rotary(const mdcnn_heads* maps, int n_maps, int tokens, int d
     while (j.group > 1 && blocks * ((heads + j.group - 1) / j.group) < 2048) j.group = (j.group + 1) / 2;
     if (j.group == 1 && heads > 65535) j.group = 2;                        // (the grid's second extent)
     return launched(launch_rotary(j, dtype, vec, interleaved != 0, (hipStream_t)stream), "rotary");
+}
+
+int mdcnn_cache_pitch(int dim) {
+    if (dim < 8 || dim > 256 || dim % 8) return 0;
+    for (int p : {32, 64, 96, 128, 192})
+        if (p >= dim) return p;
+    return 256;
+}
+
+mdcnn_status mdcnn_cache_store(const mdcnn_cache_desc* c, const mdcnn_heads* k, const mdcnn_heads* v, int tokens, const int* starts_dev, const int* held_dev, int max_new, int dtype, void* stream) {
+    return run_cache(c, k, v, tokens, starts_dev, held_dev, max_new, dtype, true, stream);
+}
+
+mdcnn_status mdcnn_cache_read(const mdcnn_cache_desc* c, const mdcnn_heads* k, const mdcnn_heads* v, int tokens, const int* starts_dev, const int* first_dev, int max_new, int dtype, void* stream) {
+    return run_cache(c, k, v, tokens, starts_dev, first_dev, max_new, dtype, false, stream);
 }
 
 }  // extern "C"

@@ -58,4 +58,24 @@ struct RotaryJob {
 };
 hipError_t launch_rotary(const RotaryJob& j, int dtype, int vec, bool interleaved, hipStream_t st);
 
+// The cache --------------------------------------------------------------------------------------------------------------
+struct CacheMap {
+    const void* x;
+    void* y;
+    long long x_token, x_head, y_token, y_head;
+};
+struct CacheJob {
+    int8_t* k_codes;
+    int8_t* v_codes;
+    float* k_scale;
+    float* v_scale;
+    const int* table;
+    const int* starts;           // [n_seq + 1]
+    const int* first;            // [n_seq] position of a sequence's first token of the call
+    CacheMap k, v;
+    int pages, heads, dim, pitch, n_seq, max_pages, max_new, tokens;
+    int slots;                   // pages that a sequence's tokens may lie in
+};
+hipError_t launch_cache(const CacheJob& j, int dtype, int vec, bool store, hipStream_t st);
+
 }  // namespace mdcnn

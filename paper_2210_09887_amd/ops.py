@@ -1,4 +1,5 @@
-"""Operators behind the feature maps, on device tensors: group norm with an activation, rotary positions.
+"""Operators behind the feature maps, on device tensors: group norm with an activation, rotary positions, a cache of
+keys and values in 8 bits.
 
 Argument marshalling only: shapes, strides and types are taken from the tensors, outputs and workspaces come from torch, the
 work is enqueued on the current stream of the tensors' device.  `group_norm_act` is the same for autograd.
@@ -182,3 +183,62 @@ class _Rotary(torch.autograd.Function):
 def rotary_turn(maps, positions, steps, axes=1, interleaved=False, magnitude=1.0):
     """`rotary` for autograd: gradients of the maps."""
     return list(_Rotary.apply(positions, steps, axes, interleaved, magnitude, *maps))
+
+
+# -- the cache --------------------------------------------------------------------------------------------------------------
+class GpuCache:
+    """Keys and values in pages of 64 tokens, 8 bits a value with one scale for each page and head.
+
+    k: int8 [pages, heads, 64, pitch], v: int8 [pages, heads, pitch, 64], pitch the next of 32, 64, 96, 128, 192, 256 to `dim`; k_scale, v_scale:
+    float32 [pages, heads].  The tensors are the caller's (`GpuCache.empty` makes them).  Which pages are whose is the caller's too: `table` int32
+    [sequences, max_pages] of the calls says in which page tokens 64 i .. 64 i + 63 of a sequence lie; entries outside the pool hold no page."""
+
+    def __init__(self, k, v, k_scale, v_scale, dim):
+        pages, heads, dev = k.shape[0], k.shape[1], k.device
+        pitch = B.mdcnn_cache_pitch(dim)
+        _need(pitch > 0, "dim: a multiple of 8 from 8 to 256")
+        _need(k.dtype == v.dtype == torch.int8 and k.shape == (pages, heads, 64, pitch) and v.shape == (pages, heads, pitch, 64), f"k, v: int8 [pages, heads, 64, {pitch}] and [pages, heads, {pitch}, 64]")
+        _need(k_scale.dtype == v_scale.dtype == torch.float32 and k_scale.shape == v_scale.shape == (pages, heads), "k_scale, v_scale: float32 [pages, heads]")
+        _need(all(t.is_contiguous() for t in (k, v, k_scale, v_scale)), "k, v, k_scale, v_scale: contiguous")
+        _on(dev, v=v, k_scale=k_scale, v_scale=v_scale)
+        self.k, self.v, self.k_scale, self.v_scale, self.dim, self.heads, self.device = k, v, k_scale, v_scale, int(dim), heads, dev
+        self._desc = (pages, heads, int(dim), k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+
+    @classmethod
+    def empty(cls, pages, heads, dim, device="cuda:0"):
+        pitch = B.mdcnn_cache_pitch(dim)
+        _need(pitch > 0, "dim: a multiple of 8 from 8 to 256")
+        codes = torch.empty((2, pages, heads, 64 * pitch), dtype=torch.int8, device=device)
+        scales = torch.empty((2, pages, heads), dtype=torch.float32, device=device)
+        return cls(codes[0].view(pages, heads, 64, pitch), codes[1].view(pages, heads, pitch, 64), scales[0], scales[1], dim)
+
+    def _cache(self, table, **per_sequence):
+        _need(table.dtype == torch.int32 and table.dim() == 2 and table.is_contiguous(), "table: contiguous int32 [sequences, max_pages]")
+        n = table.shape[0]
+        for name, t in per_sequence.items():
+            _need(t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n + (name == "starts"), f"{name}: {n + (name == 'starts')} contiguous int32 values")
+        _on(self.device, table=table, **per_sequence)
+        return B.mdcnn_cache_desc(*self._desc, table.data_ptr(), n, table.shape[1])
+
+    def _side(self, name, t):
+        _need(t.dim() == 3 and t.shape[1] == self.heads and t.shape[2] == self.dim and t.stride(2) == 1, f"{name}: [tokens, {self.heads}, {self.dim}], channels side by side")
+        return B.mdcnn_heads(t.data_ptr(), t.data_ptr(), self.heads, t.stride(0), t.stride(1), t.stride(0), t.stride(1))
+
+    def store(self, k, v, table, starts, held, max_new):
+        """Puts new tokens [tokens, heads, dim] into their pages: sequence s has tokens starts[s] .. starts[s + 1] - 1, which follow the held[s]
+        that it has already.  max_new: no sequence has more new tokens."""
+        _need(k.dtype == v.dtype and k.dtype in _DTYPE and k.shape == v.shape, "k, v: float32, float16 or bfloat16 of one shape")
+        _on(self.device, k=k, v=v)
+        c = self._cache(table, starts=starts, held=held)
+        with torch.cuda.device(self.device):
+            B.mdcnn_cache_store(c, self._side("k", k), self._side("v", v), k.shape[0], starts.data_ptr(), held.data_ptr(), max_new, _DTYPE[k.dtype], _stream(self.device))
+
+    def read(self, table, starts, first, max_new, tokens, dtype):
+        """The values of tokens first[s] .. of every sequence s, starts[s + 1] - starts[s] of them, as (k, v) [tokens, heads, dim]; tokens = starts[-1]."""
+        _need(dtype in _DTYPE, "dtype: float32, float16 or bfloat16")
+        k, v = (torch.empty((tokens, self.heads, self.dim), dtype=dtype, device=self.device) for _ in range(2))
+        c = self._cache(table, starts=starts, first=first)
+        with torch.cuda.device(self.device):
+            if tokens:
+                B.mdcnn_cache_read(c, self._side("k", k), self._side("v", v), k.shape[0], starts.data_ptr(), first.data_ptr(), max_new, _DTYPE[dtype], _stream(self.device))
+        return k, v

@@ -98,3 +98,27 @@ def test_rotary_arguments(change, status):
     kw = dict(maps=[heads()], tokens=3, dim=32, dtype=0, pos_ptr=FAKE, axes=1, steps_ptr=FAKE, turned=32)
     kw.update(change)
     refused(status, lambda: B.mdcnn_rotary(**kw))
+
+
+def cache(**kw):
+    c = B.mdcnn_cache_desc(10, 4, 32, FAKE, FAKE, FAKE, FAKE, FAKE, 3, 5)
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+def test_cache_pitch():
+    assert [B.mdcnn_cache_pitch(d) for d in (0, 4, 7, 8, 12, 32, 40, 64, 72, 96, 104, 128, 136, 192, 200, 256, 264)] == \
+        [0, 0, 0, 32, 0, 32, 64, 64, 96, 96, 128, 128, 192, 192, 256, 256, 0]
+
+
+@pytest.mark.parametrize("call", [B.mdcnn_cache_store, B.mdcnn_cache_read], ids=["store", "read"])
+@pytest.mark.parametrize("change,status", [
+    (dict(c=dict(dim=30)), 2), (dict(c=dict(heads=0)), 2), (dict(c=dict(pages=-1)), 5), (dict(c=dict(n_seq=-1)), 5), (dict(c=dict(max_pages=-1)), 5), (dict(c=dict(k_dev=None)), 1),
+    (dict(c=dict(v_scale_dev=None)), 1), (dict(c=dict(table_dev=None)), 1), (dict(c=dict(v_dev=FAKE + 8)), 4), (dict(c=dict(table_dev=FAKE + 2)), 4), (dict(dtype=3), 3),
+    (dict(max_new=-1), 2), (dict(tokens=-1), 2), (dict(starts=None), 1), (dict(at=None), 1), (dict(starts=FAKE + 1), 4), (dict(at=FAKE + 2), 4), (dict(k=dict(heads=3)), 2),
+    (dict(v=dict(x_dev=None, y_dev=None)), 1), (dict(k=dict(x_dev=FAKE + 1, y_dev=FAKE + 1)), 4), (dict(c=dict(n_seq=1 << 20), max_new=1 << 30, tokens=1 << 30), 5)])
+def test_cache_arguments(call, change, status):
+    kw = dict(dtype=1, max_new=100, tokens=200, starts=FAKE, at=FAKE)
+    kw.update({k: v for k, v in change.items() if k not in ("c", "k", "v")})
+    refused(status, call, cache(**change.get("c", {})), heads(**change.get("k", {})), heads(**change.get("v", {})), kw["tokens"], kw["starts"], kw["at"], kw["max_new"], kw["dtype"])
