@@ -711,6 +711,28 @@ mdcnn_status mdcnn_cache_read(const mdcnn_cache_desc* c, const mdcnn_heads* k, c
                               const int* starts_dev, const int* first_dev, int max_new, int dtype,
                               void* stream);
 
+/* Attention of queries over such a cache.  Sequence s has the queries starts_dev[s] .. starts_dev[s + 1] - 1 and
+ * lengths_dev[s] tokens in the cache.  q->heads is a multiple of the cache's heads: query head h reads head h / (q->heads / heads).
+ *   out = sum_j p_j v_j,  p = softmax over the tokens j that the query sees of scale q . k_j
+ * A query sees every token of its sequence that has a page and, where a mask is given, a nonzero byte in it.  causal: query i of n is the token
+ * lengths - n + i and sees nothing behind itself; window > 0 (causal only): only the `window` tokens up to itself.  A query that sees
+ * nothing gets zeros and a log-sum of minus infinity; hidden tokens have no influence whatever their page holds. */
+typedef struct {
+    const int* starts_dev;    /* n_seq + 1                                              */
+    const int* lengths_dev;   /* n_seq                                                  */
+    int tokens;               /* queries in all: starts_dev[n_seq]                      */
+    int max_new, max_len;     /* no sequence has more queries / more tokens in the cache */
+    float scale;
+    int causal, window;
+    const uint8_t* mask_dev;  /* n_seq rows of mask_row bytes, byte j: token j; or NULL  */
+    long long mask_row;       /* >= max_len                                             */
+} mdcnn_attend_desc;
+mdcnn_status mdcnn_cache_attend_bytes(const mdcnn_cache_desc* c, const mdcnn_attend_desc* a, int q_heads,
+                                      size_t* bytes);
+/* q: queries and output (x and y), dtype f32, f16 or bf16; lse_dev: tokens * q->heads floats, natural logarithm, or NULL. */
+mdcnn_status mdcnn_cache_attend(const mdcnn_cache_desc* c, const mdcnn_attend_desc* a, const mdcnn_heads* q,
+                                int dtype, float* lse_dev, void* work_dev, size_t work_bytes, void* stream);
+
 const char* mdcnn_last_error(void);
 const char* mdcnn_version(void);
 

@@ -35,7 +35,7 @@ EXPORTS = ["mdcnn_conv_border", "mdcnn_conv_tiles", "mdcnn_rect_tiles", "mdcnn_g
            "mdcnn_shift_camera", "mdcnn_set_crop", "mdcnn_layer_forward", "mdcnn_layer_forward_noalloc", "mdcnn_net_create", "mdcnn_net_destroy",
            "mdcnn_frame", "mdcnn_frame_crop", "mdcnn_frame_batch", "mdcnn_frame_batch_crop", "mdcnn_frame_plan", "mdcnn_frames", "mdcnn_frames_batch", "mdcnn_frames_crop", "mdcnn_frames_masked", "mdcnn_frames_plan", "mdcnn_frames_rounds", "mdcnn_input_mask", "mdcnn_read_view", "mdcnn_write_view", "mdcnn_set_option", "mdcnn_profile_read", "mdcnn_profile_read_launches", "mdcnn_bench_copy", "mdcnn_bench_mfma",
            "mdcnn_pack_weights", "mdcnn_group_norm_bytes", "mdcnn_group_norm", "mdcnn_group_norm_backward", "mdcnn_rotary_table", "mdcnn_rotary", "mdcnn_cache_pitch",
-           "mdcnn_cache_store", "mdcnn_cache_read", "mdcnn_last_error", "mdcnn_version"]
+           "mdcnn_cache_store", "mdcnn_cache_read", "mdcnn_cache_attend_bytes", "mdcnn_cache_attend", "mdcnn_last_error", "mdcnn_version"]
 
 
 class mdcnn_buffer_desc(C.Structure):
@@ -78,6 +78,11 @@ class mdcnn_heads(C.Structure):
 class mdcnn_cache_desc(C.Structure):
     _fields_ = [("pages", C.c_int), ("heads", C.c_int), ("dim", C.c_int), ("k_dev", C.c_void_p), ("v_dev", C.c_void_p), ("k_scale_dev", C.c_void_p),
                 ("v_scale_dev", C.c_void_p), ("table_dev", C.c_void_p), ("n_seq", C.c_int), ("max_pages", C.c_int)]
+
+
+class mdcnn_attend_desc(C.Structure):
+    _fields_ = [("starts_dev", C.c_void_p), ("lengths_dev", C.c_void_p), ("tokens", C.c_int), ("max_new", C.c_int), ("max_len", C.c_int), ("scale", C.c_float),
+                ("causal", C.c_int), ("window", C.c_int), ("mask_dev", C.c_void_p), ("mask_row", C.c_longlong)]
 
 
 class MdcnnError(RuntimeError):
@@ -141,6 +146,8 @@ def lib():
         hs, cd = C.POINTER(mdcnn_heads), C.POINTER(mdcnn_cache_desc)
         L.mdcnn_cache_store.argtypes = [cd, hs, hs, C.c_int, vp, vp, C.c_int, C.c_int, vp]
         L.mdcnn_cache_read.argtypes = [cd, hs, hs, C.c_int, vp, vp, C.c_int, C.c_int, vp]
+        L.mdcnn_cache_attend_bytes.argtypes = [cd, C.POINTER(mdcnn_attend_desc), C.c_int, C.POINTER(sz)]
+        L.mdcnn_cache_attend.argtypes = [cd, C.POINTER(mdcnn_attend_desc), hs, C.c_int, vp, vp, sz, vp]
         L.mdcnn_last_error.restype = C.c_char_p
         L.mdcnn_version.restype = C.c_char_p
         for name in EXPORTS:
@@ -459,3 +466,13 @@ def mdcnn_cache_store(cache: mdcnn_cache_desc, k: mdcnn_heads, v: mdcnn_heads, t
 
 def mdcnn_cache_read(cache: mdcnn_cache_desc, k: mdcnn_heads, v: mdcnn_heads, tokens: int, starts_ptr, first_ptr, max_new: int, dtype: int, stream: int = 0):
     _check(lib().mdcnn_cache_read(C.byref(cache), C.byref(k), C.byref(v), tokens, starts_ptr, first_ptr, max_new, dtype, stream))
+
+
+def mdcnn_cache_attend_bytes(cache: mdcnn_cache_desc, how: mdcnn_attend_desc, q_heads: int) -> int:
+    n = C.c_size_t()
+    _check(lib().mdcnn_cache_attend_bytes(C.byref(cache), C.byref(how), q_heads, C.byref(n)))
+    return n.value
+
+
+def mdcnn_cache_attend(cache: mdcnn_cache_desc, how: mdcnn_attend_desc, q: mdcnn_heads, dtype: int, lse_ptr, work_ptr, work_bytes: int, stream: int = 0):
+    _check(lib().mdcnn_cache_attend(C.byref(cache), C.byref(how), C.byref(q), dtype, lse_ptr, work_ptr, work_bytes, stream))

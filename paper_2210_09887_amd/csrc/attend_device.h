@@ -1,0 +1,85 @@
+// What the attention kernels share: which tokens a row sees, codes as matrix operands, queries as such.
+//
+// Rows.  The queries of a sequence that read one head of the cache - n queries of g heads each - are n g rows: row r is query
+// r / g, head r % g of the group.  Every kernel computes S' = K Q' (tokens by rows) and O' = V' P', so that a lane holds tokens of
+// one row: maxima and sums over tokens stay in the lane but for two or one steps, and P' leaves the first product in the registers in which
+// the second takes it.  Which token a row of an instruction is is free as long as both products agree: lanes get runs of
+// neighbouring tokens, which is how the values lie in a page.
+//
+// Codes become halves without a conversion: a byte c + 128 in the low byte of 0x6400 is the half 1152 + c, minus 1152 is c,
+// exactly.  Scales are multiplied in where the sums are: that of the keys with the logits, that of the values with the probabilities,
+// relative to the largest one so far (so that halves hold them whatever their size).
+#pragma once
+
+#include "ops_device.h"
+#include "ops_internal.h"
+
+namespace mdcnn {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef unsigned uint4v __attribute__((ext_vector_type(4)));
+typedef unsigned uint2v __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2E = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// Eight codes as halves.
+__device__ __forceinline__ half8 halves_of(unsigned a, unsigned b) {
+    union { unsigned u[4]; half2v h[4]; half8 v; } r;
+    a ^= 0x80808080u;
+    b ^= 0x80808080u;
+    r.u[0] = __builtin_amdgcn_perm(0x64646464u, a, 0x04010400u);
+    r.u[1] = __builtin_amdgcn_perm(0x64646464u, a, 0x04030402u);
+    r.u[2] = __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u);
+    r.u[3] = __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u);
+    const half2v off = {(_Float16)1152, (_Float16)1152};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.h[i] -= off;
+    return r.v;
+}
+
+// Sequence of a block and what its rows see.
+struct Rows {
+    int len, n, rows;            // tokens in the cache, queries, rows (queries x group)
+    long long q0;                // first query of the sequence in the maps
+    __device__ __forceinline__ bool load(const AttendJob& j, int seq) {
+        const int s0 = j.starts[seq];
+        n = min(min(j.starts[seq + 1], j.tokens) - s0, j.max_new);
+        if (s0 < 0 || n <= 0) return false;
+        len = max(0, min(j.lengths[seq], j.max_len));
+        q0 = s0;
+        rows = n * j.group;
+        return true;
+    }
+    // positions that query i sees: lo <= position < hi
+    __device__ __forceinline__ int hi(const AttendJob& j, int i) const { return j.causal ? min(len, max(0, len - n + i + 1)) : len; }
+    __device__ __forceinline__ int lo(const AttendJob& j, int i) const { return j.window ? max(0, len - n + i + 1 - j.window) : 0; }
+};
+
+// The power of two that brings the largest magnitude of a row to 2^13 .. 2^14 (1 for none, or one that is not finite).
+__device__ __forceinline__ int exponent_of(float top) {
+    const int e = (int)(__float_as_uint(top) >> 23);
+    return top > 0.f && e < 255 ? e - 127 - 13 : 0;
+}
+__device__ __forceinline__ float scaled(float x, int e) { return ldexpf(x, e); }
+
+// Which of 16 tokens from `pos` on have a nonzero byte, as bits.
+__device__ __forceinline__ unsigned mask_bits(const uint8_t* row, int pos, int end, bool whole) {
+    unsigned bits = 0;
+    if (whole && pos + 16 <= end) {
+        const uint4v w = *(const uint4v*)(row + pos);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) bits |= (w[i] >> (8 * e) & 0xff ? 1u : 0u) << (4 * i + e);
+    } else {
+        for (int i = 0; i < 16; ++i)
+            if (pos + i < end && row[pos + i]) bits |= 1u << i;
+    }
+    return bits;
+}
+
+}  // namespace mdcnn

@@ -1,0 +1,319 @@
+// Attention over a cache of 8-bit pages, rows by sixteen: single tokens, a few queries, anything (the tiles of prompts and frames:
+// kernels_attend_tiles.hip).
+//
+// With few rows the cache's bytes bound it: each is read once, 16 bytes a lane, straight into the registers of the wave that multiplies
+// them; the next page's keys are on their way while the softmax and the values of this one are worked on, and the other way
+// round.  A wave has pages of its own (every fourth of its block's run) with a maximum and a sum of its own; the four are joined
+// in LDS.  Runs of pages are split over blocks where rows alone would not fill the GPU, and joined by a second launch.
+#include "attend_device.h"
+
+namespace mdcnn {
+
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kPage = MDCNN_PAGE_TOKENS;
+
+// Place of a block: split fastest, then the tile of rows.
+struct AttendBlock {
+    int split, tile, head, seq;
+    __device__ __forceinline__ AttendBlock(const AttendJob& j, unsigned b) {
+        split = b % j.splits;
+        b /= j.splits;
+        tile = b % j.tiles;
+        b /= j.tiles;
+        head = b % j.heads;
+        seq = b / j.heads;
+    }
+};
+
+// Pages of a block: those of the rows r0 .. r1 - 1, of which split z has the run [first, last).
+struct Run {
+    int first, last, splits;
+    __device__ __forceinline__ Run(const AttendJob& j, const Rows& s, int r0, int r1, int z) {
+        const int lo = s.lo(j, r0 / j.group), hi = s.hi(j, (r1 - 1) / j.group);
+        const int p0 = lo / kPage, p1 = min((hi + kPage - 1) / kPage, j.max_pages);
+        splits = max(0, (p1 - p0 + j.run - 1) / j.run);
+        first = p0 + z * j.run;
+        last = min(p1, first + j.run);
+    }
+};
+
+template <typename T, int DP>
+__global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(AttendJob j) {
+    constexpr bool kTwo = sizeof(T) == 4;                  // fp32 queries and probabilities as sums of two halves
+    constexpr int NS = DP / 32, NV = DP / 16;              // steps of 32 channels, tiles of 16
+    constexpr int U = DP / 64;                             // pairs of steps that a 16-byte load serves
+    __shared__ float s_top[kWaves][16], s_sum[kWaves][16];
+    __shared__ __align__(16) float s_out[kWaves][16][DP + 4];
+    const AttendBlock blk(j, blockIdx.x);
+    const int head = blk.head, seq = blk.seq;
+    Rows s;
+    if (!s.load(j, seq)) return;
+    const int r0 = blk.tile * 16, r1 = min(r0 + 16, s.rows);
+    if (r0 >= s.rows) return;
+    const Run run(j, s, r0, r1, blk.split);
+    if (blk.split > 0 && run.first >= run.last) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, quad = lane >> 4;
+
+    // Queries of this lane's row, channels in the order in which the keys are loaded.
+    const int row = r0 + n, query = row / j.group;
+    const bool live = row < s.rows;
+    const T* q = (const T*)j.q + (s.q0 + (live ? query : 0)) * j.q_token + (long long)(head * j.group + (live ? row % j.group : 0)) * j.q_head;
+    half8 qh[NS], ql[kTwo ? NS : 1];
+    int e;
+    {
+        float f[NS][8], top = 0.f;
+#pragma unroll
+        for (int st = 0; st < NS; ++st)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = (st < 2 * U ? 64 * (st / 2) + 16 * quad + 8 * (st & 1) : 64 * U + 8 * quad) + i;
+                f[st][i] = live && c < j.dim ? to_f32(q[c]) : 0.f;
+                top = fmaxf(top, fabsf(f[st][i]));
+            }
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        e = exponent_of(top);
+#pragma unroll
+        for (int st = 0; st < NS; ++st)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float x = scaled(f[st][i], -e);
+                qh[st][i] = (_Float16)x;
+                if constexpr (kTwo) ql[st][i] = (_Float16)(x - (float)qh[st][i]);
+            }
+    }
+    const float logit = scaled(j.scale * kLog2E, e);
+    const int hi = live ? s.hi(j, query) : 0, lo = live ? s.lo(j, query) : 0;
+    const int all_hi = s.hi(j, r0 / j.group), all_lo = s.lo(j, (r1 - 1) / j.group);      // seen by every row
+    const uint8_t* mask = j.mask ? j.mask + seq * j.mask_row : nullptr;
+
+    float top = -INFINITY, sum = 0.f, ref = 0.f;           // maximum and sum of this lane's row, largest scale of the values
+    float4v out[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) out[v] = float4v{0.f, 0.f, 0.f, 0.f};
+
+    const int* table = j.table + (long long)seq * j.max_pages;
+    const int per_head = kPage * DP;
+    uint4v kr[4][U ? U : 1];
+    uint2v kx[4];
+    uint4v vr[NV];
+    auto page_at = [&](int p) {
+        const int id = p < run.last ? table[p] : -1;
+        return id >= 0 && id < j.pages ? id : -1;
+    };
+    // (no page: what the first one holds, which is then not looked at; there is one wherever there is a run)
+    auto load_keys = [&](int id) {
+        const int8_t* k = j.k_codes + ((long long)max(id, 0) * j.heads + head) * per_head;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int8_t* r = k + (16 * (n >> 2) + 4 * t + (n & 3)) * DP;
+#pragma unroll
+            for (int u = 0; u < U; ++u) kr[t][u] = *(const uint4v*)(r + 64 * u + 16 * quad);
+            if constexpr (DP % 64 != 0) kx[t] = *(const uint2v*)(r + 64 * U + 8 * quad);
+        }
+    };
+    auto load_values = [&](int id) {
+        const int8_t* v = j.v_codes + ((long long)max(id, 0) * j.heads + head) * per_head;
+#pragma unroll
+        for (int t = 0; t < NV; ++t) vr[t] = *(const uint4v*)(v + (16 * t + n) * kPage + 16 * quad);
+    };
+    int p = run.first + wave, id = page_at(p), next = page_at(p + kWaves);
+    if (p < run.last) {
+        load_keys(id);
+        load_values(id);
+    }
+    for (; p < run.last; p += kWaves) {
+        const int after = page_at(p + 2 * kWaves);
+        if (id < 0) {                                      // no page: its tokens do not exist
+            id = next;
+            next = after;
+            load_keys(id);
+            load_values(id);
+            continue;
+        }
+        const long long at = (long long)id * j.heads + head;
+        const float ks = j.k_scale[at], vs = j.v_scale[at];
+        float4v acc[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            acc[t] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int st = 0; st < NS; ++st) {
+                const half8 k = st < 2 * U ? (st & 1 ? halves_of(kr[t][st / 2][2], kr[t][st / 2][3]) : halves_of(kr[t][st / 2][0], kr[t][st / 2][1])) : halves_of(kx[t][0], kx[t][1]);
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qh[st], acc[t], 0, 0, 0);
+                if constexpr (kTwo) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, ql[st], acc[t], 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);             // or all codes are made halves first, in as many registers
+        }
+        load_keys(next);
+        // logits in powers of two; hidden ones minus infinity
+        const float by = logit * ks;
+        float x[16];
+#pragma unroll
+        for (int t = 0; t < 16; ++t) x[t] = acc[t / 4][t % 4] * by;
+        unsigned seen = 0xffffu;
+        const int pos = p * kPage + 16 * quad;
+        if (p * kPage < all_lo || (p + 1) * kPage > all_hi || mask) {
+            if (mask) seen = mask_bits(mask, pos, s.len, j.mask_whole);
+#pragma unroll
+            for (int t = 0; t < 16; ++t) {
+                if (pos + t < lo || pos + t >= hi) seen &= ~(1u << t);
+                x[t] = seen >> t & 1 ? x[t] : -INFINITY;
+            }
+        }
+        float m = x[0];
+#pragma unroll
+        for (int t = 1; t < 16; ++t) m = fmaxf(m, x[t]);
+        m = fmaxf(m, __shfl_xor(m, 16, 64));
+        m = fmaxf(m, __shfl_xor(m, 32, 64));
+        m = fmaxf(m, top);
+        const float base = m == -INFINITY ? 0.f : m;       // (nothing seen so far: all probabilities come out as zeros)
+        const float fade = exp2_fast(top - base);
+        top = m;
+        float fade_out = fade, rel;                        // scale of the values relative to the largest so far
+        if (vs <= ref) {
+            rel = ref > 0.f ? vs / ref : 0.f;
+        } else if (vs == vs) {
+            fade_out *= ref / vs;
+            ref = vs;
+            rel = 1.f;
+        } else {
+            rel = vs;                                      // not a number: the tokens that are seen make the row one
+        }
+        float add = 0.f;
+        half8 ph[2], pl[kTwo ? 2 : 1];
+#pragma unroll
+        for (int t = 0; t < 16; ++t) {
+            const float w = exp2_fast(x[t] - base);
+            add += w;
+            const float y = seen >> t & 1 ? w * rel : 0.f;
+            ph[t / 8][t % 8] = (_Float16)y;
+            if constexpr (kTwo) pl[t / 8][t % 8] = (_Float16)(y - (float)ph[t / 8][t % 8]);
+        }
+        sum = sum * fade + add;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            out[v] *= fade_out;
+            const half8 a = halves_of(vr[v][0], vr[v][1]), b = halves_of(vr[v][2], vr[v][3]);
+            out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, ph[0], out[v], 0, 0, 0);
+            out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, ph[1], out[v], 0, 0, 0);
+            if constexpr (kTwo) {
+                out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, pl[0], out[v], 0, 0, 0);
+                out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, pl[1], out[v], 0, 0, 0);
+            }
+            if (v % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+        id = next;
+        next = after;
+        load_values(id);
+    }
+    // join the four waves
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    if (quad == 0) { s_top[wave][n] = top; s_sum[wave][n] = sum; }
+#pragma unroll
+    for (int v = 0; v < NV; ++v) *(float4v*)&s_out[wave][n][16 * v + 4 * quad] = out[v] * ref;
+    __syncthreads();
+    const int m = threadIdx.x / 16, c0 = threadIdx.x % 16;
+    if (r0 + m >= s.rows) return;
+    float peak = s_top[0][m], total = 0.f, weight[kWaves];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) peak = fmaxf(peak, s_top[w][m]);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        weight[w] = exp2_fast(s_top[w][m] - (peak == -INFINITY ? 0.f : peak));
+        total += weight[w] * s_sum[w][m];
+    }
+    const bool whole = run.splits <= 1;
+    const int r = r0 + m;
+    const long long slot = (((long long)seq * j.heads + head) * j.tiles + blk.tile) * j.splits + blk.split;
+    T* y = (T*)j.y + (s.q0 + r / j.group) * j.y_token + (long long)(head * j.group + r % j.group) * j.y_head;
+    const float inv = peak == -INFINITY && total == 0.f ? 0.f : 1.f / total;
+    for (int c = c0; c < DP; c += 16) {
+        float x = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) x += weight[w] * s_out[w][m][c];
+        if (!whole) j.part_out[(slot * 16 + m) * DP + c] = x;
+        else if (c < j.dim) y[c] = (T)(x * inv);
+    }
+    if (c0 == 0) {
+        if (!whole) j.part_top[slot * 16 + m] = float2{peak, total};
+        else if (j.lse) j.lse[(s.q0 + r / j.group) * (j.heads * j.group) + head * j.group + r % j.group] = kLn2 * (peak + __log2f(total));
+    }
+}
+
+// Joins the splits of a row; a block to a row: threads over its channels, four of them each, and over the splits.
+template <typename T, int DP>
+__global__ __launch_bounds__(kThreads) void k_attend_join(AttendJob j) {
+    constexpr int kLanes = DP / 4, kSets = kThreads / kLanes;
+    __shared__ float4v s_part[kSets][kLanes];
+    __shared__ float s_sum[kSets];
+    const int per = j.max_new * j.group;
+    const int r = blockIdx.x % per, head = blockIdx.x / per % j.heads, seq = blockIdx.x / per / j.heads;
+    Rows s;
+    if (!s.load(j, seq) || r >= s.rows) return;
+    const int tile = r / 16, m = r % 16;
+    const Run run(j, s, tile * 16, min(tile * 16 + 16, s.rows), 0);
+    if (run.splits <= 1) return;
+    const long long slot = (((long long)seq * j.heads + head) * j.tiles + tile) * j.splits;
+    float peak = -INFINITY;
+    for (int z = threadIdx.x & 63; z < run.splits; z += 64) peak = fmaxf(peak, j.part_top[(slot + z) * 16 + m].x);
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) peak = fmaxf(peak, __shfl_xor(peak, k, 64));
+    const float base = peak == -INFINITY ? 0.f : peak;
+    const int set = threadIdx.x / kLanes, c = threadIdx.x % kLanes;
+    if (set < kSets) {
+        float4v x = float4v{0.f, 0.f, 0.f, 0.f};
+        float total = 0.f;
+#pragma unroll 4
+        for (int z = set; z < run.splits; z += kSets) {
+            const float2 t = j.part_top[(slot + z) * 16 + m];
+            const float w = exp2_fast(t.x - base);
+            total += w * t.y;
+            x += w * *(const float4v*)(j.part_out + ((slot + z) * 16 + m) * DP + 4 * c);
+        }
+        s_part[set][c] = x;
+        if (c == 0) s_sum[set] = total;
+    }
+    __syncthreads();
+    if (set) return;
+    float4v x = s_part[0][c];
+    float total = s_sum[0];
+    for (int k = 1; k < kSets; ++k) { x += s_part[k][c]; total += s_sum[k]; }
+    const float inv = peak == -INFINITY && total == 0.f ? 0.f : 1.f / total;
+    T* y = (T*)j.y + (s.q0 + r / j.group) * j.y_token + (long long)(head * j.group + r % j.group) * j.y_head;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (4 * c + i < j.dim) y[4 * c + i] = (T)(x[i] * inv);
+    if (c == 0 && j.lse) j.lse[(s.q0 + r / j.group) * (j.heads * j.group) + head * j.group + r % j.group] = kLn2 * (peak + __log2f(total));
+}
+
+template <typename T, int DP>
+hipError_t launch(const AttendJob& j, hipStream_t st) {
+    k_attend_rows<T, DP><<<(unsigned)((long long)j.splits * j.tiles * j.n_seq * j.heads), kThreads, 0, st>>>(j);
+    if (j.splits > 1) k_attend_join<T, DP><<<(unsigned)((long long)j.max_new * j.group * j.n_seq * j.heads), kThreads, 0, st>>>(j);
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_of(const AttendJob& j, hipStream_t st) {
+    switch (j.pitch) {
+        case 32: return launch<T, 32>(j, st);
+        case 64: return launch<T, 64>(j, st);
+        case 96: return launch<T, 96>(j, st);
+        case 128: return launch<T, 128>(j, st);
+        case 192: return launch<T, 192>(j, st);
+        default: return launch<T, 256>(j, st);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_attend_rows(const AttendJob& j, int dtype, hipStream_t st) {
+    if (dtype == MDCNN_F32) return launch_of<float>(j, st);
+    if (dtype == MDCNN_F16) return launch_of<_Float16>(j, st);
+    return launch_of<__bf16>(j, st);
+}
+
+}  // namespace mdcnn

@@ -214,6 +214,41 @@ mdcnn_status run_cache(const mdcnn_cache_desc* c, const mdcnn_heads* k, const md
     return launched(launch_cache(j, dtype, vec, store, (hipStream_t)stream), call);
 }
 
+// ---- attention ------------------------------------------------------------------------------------------------------------
+mdcnn_status check_attend(const mdcnn_cache_desc* c, const mdcnn_attend_desc* a, int q_heads) {
+    const mdcnn_status st = check_cache(c, "cache_attend");
+    if (st) return st;
+    if (!a) return fail(MDCNN_ERR_NULL, "cache_attend: description is NULL");
+    if (q_heads < 1 || q_heads % c->heads || q_heads > 65535) return fail(MDCNN_ERR_SHAPE, "cache_attend: %d query heads over %d", q_heads, c->heads);
+    if (a->tokens < 0 || a->max_new < 0 || a->max_len < 0) return fail(MDCNN_ERR_SHAPE, "cache_attend: negative sizes");
+    if ((a->causal & ~1) || a->window < 0 || (a->window && !a->causal)) return fail(MDCNN_ERR_SHAPE, "cache_attend: causal is 0 or 1, a window needs it");
+    if (!std::isfinite(a->scale)) return fail(MDCNN_ERR_SHAPE, "cache_attend: scale is not finite");
+    if (c->n_seq && (!a->starts_dev || !a->lengths_dev)) return fail(MDCNN_ERR_NULL, "cache_attend: starts or lengths are NULL");
+    if (!aligned(a->starts_dev, 4) || !aligned(a->lengths_dev, 4)) return fail(MDCNN_ERR_ALIGN, "cache_attend: starts or lengths are misaligned");
+    if (a->mask_dev && a->mask_row < a->max_len) return fail(MDCNN_ERR_SIZE, "cache_attend: mask rows of %lld bytes, %d tokens", a->mask_row, a->max_len);
+    return MDCNN_OK;
+}
+
+// Tiles of 16 rows, and pages to a split: blocks for four to a compute unit, runs of 4 to 32 pages (a wave has a quarter of them).
+mdcnn_status plan_attend(const mdcnn_cache_desc& c, const mdcnn_attend_desc& a, int q_heads, AttendJob& j, size_t* bytes) {
+    j.pages = c.pages; j.heads = c.heads; j.group = q_heads / c.heads; j.dim = c.dim; j.pitch = mdcnn_cache_pitch(c.dim);
+    j.n_seq = c.n_seq; j.max_pages = c.pages ? c.max_pages : 0;
+    j.tokens = a.tokens; j.max_new = std::min(a.max_new, a.tokens); j.max_len = a.max_len;
+    j.causal = a.causal; j.window = a.window; j.scale = a.scale;
+    const long long rows = (long long)j.max_new * j.group, columns = (rows + 15) / 16 * c.n_seq * c.heads;
+    if (rows > 0x7fffffffll || rows * c.n_seq * c.heads > 0x7fffffffll) return fail(MDCNN_ERR_SIZE, "cache_attend: too many rows");
+    j.tiles = (int)((rows + 15) / 16);
+    long long most = std::min<long long>((a.max_len + (long long)MDCNN_PAGE_TOKENS - 1) / MDCNN_PAGE_TOKENS, c.max_pages);
+    if (a.window) most = std::min<long long>(most, (a.window + (long long)j.max_new + 2 * MDCNN_PAGE_TOKENS - 2) / MDCNN_PAGE_TOKENS);
+    most = std::max(most, 1ll);
+    j.run = (int)std::min(32ll, std::max(4ll, columns ? most * columns / 1024 : 1ll));
+    j.splits = (int)((most + j.run - 1) / j.run);
+    if (columns >= 2048) { j.splits = 1; j.run = 1 << 30; }
+    if (columns * j.splits > 0x7fffffffll) return fail(MDCNN_ERR_SIZE, "cache_attend: too large");
+    *bytes = j.splits > 1 ? (size_t)columns * j.splits * 16 * (8 + 4 * (size_t)j.pitch) + 256 : 0;
+    return MDCNN_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -327,6 +362,39 @@ mdcnn_status mdcnn_cache_store(const mdcnn_cache_desc* c, const mdcnn_heads* k, 
 
 mdcnn_status mdcnn_cache_read(const mdcnn_cache_desc* c, const mdcnn_heads* k, const mdcnn_heads* v, int tokens, const int* starts_dev, const int* first_dev, int max_new, int dtype, void* stream) {
     return run_cache(c, k, v, tokens, starts_dev, first_dev, max_new, dtype, false, stream);
+}
+
+mdcnn_status mdcnn_cache_attend_bytes(const mdcnn_cache_desc* c, const mdcnn_attend_desc* a, int q_heads, size_t* bytes) {
+    mdcnn_status st = check_attend(c, a, q_heads);
+    if (st) return st;
+    if (!bytes) return fail(MDCNN_ERR_NULL, "cache_attend_bytes: bytes is NULL");
+    AttendJob j{};
+    return plan_attend(*c, *a, q_heads, j, bytes);
+}
+
+mdcnn_status mdcnn_cache_attend(const mdcnn_cache_desc* c, const mdcnn_attend_desc* a, const mdcnn_heads* q, int dtype, float* lse_dev, void* work_dev, size_t work_bytes, void* stream) {
+    if (!q) return fail(MDCNN_ERR_NULL, "cache_attend: queries are NULL");
+    mdcnn_status st = check_attend(c, a, q->heads);
+    if (st) return st;
+    if (!known_dtype(dtype)) return fail(MDCNN_ERR_DTYPE, "cache_attend: unknown dtype %d", dtype);
+    AttendJob j{};
+    size_t need = 0;
+    st = plan_attend(*c, *a, q->heads, j, &need);
+    if (st) return st;
+    if (!c->n_seq || !a->tokens || !a->max_new) return MDCNN_OK;
+    st = check_heads(*q, "cache_attend", "the queries", c->dim, a->tokens, storage_bytes(dtype), true, true);
+    if (st) return st;
+    if (!aligned(lse_dev, 4) || !aligned(work_dev, 16)) return fail(MDCNN_ERR_ALIGN, "cache_attend: misaligned pointer");
+    if (work_bytes < need) return fail(MDCNN_ERR_SIZE, "cache_attend: workspace of %zu bytes, %zu needed", work_bytes, need);
+    if (need && !work_dev) return fail(MDCNN_ERR_NULL, "cache_attend: workspace is NULL");
+    j.q = q->x_dev; j.y = q->y_dev; j.lse = lse_dev;
+    j.q_token = q->x_token; j.q_head = q->x_head; j.y_token = q->y_token; j.y_head = q->y_head;
+    j.k_codes = c->k_dev; j.v_codes = c->v_dev; j.k_scale = c->k_scale_dev; j.v_scale = c->v_scale_dev; j.table = c->table_dev;
+    j.starts = a->starts_dev; j.lengths = a->lengths_dev; j.mask = a->mask_dev; j.mask_row = a->mask_row;
+    j.mask_whole = aligned(a->mask_dev, 16) && (c->n_seq == 1 || a->mask_row % 16 == 0);
+    j.part_out = (float*)work_dev;
+    j.part_top = (float2*)((char*)work_dev + (size_t)j.n_seq * j.heads * j.tiles * j.splits * 16 * j.pitch * 4);
+    return launched(launch_attend_rows(j, dtype, (hipStream_t)stream), "cache_attend");
 }
 
 }  // extern "C"

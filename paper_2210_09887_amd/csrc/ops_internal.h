@@ -78,4 +78,28 @@ struct CacheJob {
 };
 hipError_t launch_cache(const CacheJob& j, int dtype, int vec, bool store, hipStream_t st);
 
+// Attention over the cache -----------------------------------------------------------------------------------------------
+struct AttendJob {
+    const void* q;
+    void* y;
+    float* lse;
+    const int8_t* k_codes;
+    const int8_t* v_codes;
+    const float* k_scale;
+    const float* v_scale;
+    const int* table;
+    const int* starts;
+    const int* lengths;
+    const uint8_t* mask;
+    float2* part_top;            // [seq][head][tile][split][16]: maximum and sum of a row
+    float* part_out;             // [..][16][pitch]
+    long long q_token, q_head, y_token, y_head, mask_row;
+    int pages, heads, group, dim, pitch, n_seq, max_pages;   // group: query heads to a head of the cache
+    int tokens, max_new, max_len, causal, window;
+    int mask_whole;              // rows of the mask begin on 16 bytes
+    int tiles, splits, run;      // tiles of rows and splits of a sequence and head (bounds), pages to a split
+    float scale;
+};
+hipError_t launch_attend_rows(const AttendJob& j, int dtype, hipStream_t st);
+
 }  // namespace mdcnn

@@ -1,5 +1,5 @@
 """Operators behind the feature maps, on device tensors: group norm with an activation, rotary positions, a cache of
-keys and values in 8 bits.
+keys and values in 8 bits and the attention that reads it.
 
 Argument marshalling only: shapes, strides and types are taken from the tensors, outputs and workspaces come from torch, the
 work is enqueued on the current stream of the tensors' device.  `group_norm_act` is the same for autograd.
@@ -34,6 +34,11 @@ def _floats(name, t, n):
     _need(t is None or (t.dtype == torch.float32 and t.numel() == n and t.is_contiguous()), f"{name}: {n} contiguous float32 values")
 
 
+def _beside(t):
+    """The last extent's elements lie side by side."""
+    return t.stride(-1) == 1 or t.shape[-1] == 1 or t.numel() == 0
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -46,7 +51,7 @@ def _work(nbytes, dev):
 def _map(name, t, like=None):
     _need(t.dim() == 4 and (like is None or t.shape == like.shape), f"{name}: a map [N, H, W, C]" + ("" if like is None else f" of shape {tuple(like.shape)}"))
     _need(t.dtype in _DTYPE and (like is None or t.dtype == like.dtype), f"{name}: float32, float16 or bfloat16" + ("" if like is None else ", as x"))
-    _need(t.stride(3) == 1 or t.shape[3] == 1, f"{name}: channels last")
+    _need(_beside(t), f"{name}: channels last")
     return B.mdcnn_strides(t.stride(0), t.stride(1), t.stride(2))
 
 
@@ -108,7 +113,7 @@ class _GroupNormAct(torch.autograd.Function):
     def backward(ctx, dy):
         x, gamma, beta, mean, rstd = ctx.saved_tensors
         groups, act = ctx.how
-        if dy.stride(3) != 1 and dy.shape[3] != 1:
+        if not _beside(dy):
             dy = dy.contiguous()
         dx, dgamma, dbeta = group_norm_backward(x, dy, mean, rstd, groups, gamma, beta, act)
         return dx, None, None if gamma is None else dgamma, None if beta is None else dbeta, None, None
@@ -137,7 +142,7 @@ def rotary_steps(turned, axes=1, base=10000.0, scaling="none", factor=1.0, origi
 def _heads(name, t, dtype, dim, tokens):
     _need(t.dim() == 3 and t.shape[0] == tokens and t.shape[2] == dim, f"{name}: [{tokens}, heads, {dim}]")
     _need(t.dtype == dtype, f"{name}: {dtype}")
-    _need(t.stride(2) == 1 or dim == 1, f"{name}: channels side by side")
+    _need(_beside(t), f"{name}: channels side by side")
 
 
 def rotary(maps, positions, steps, axes=1, interleaved=False, magnitude=1.0, inverse=False, out=None):
@@ -176,7 +181,7 @@ class _Rotary(torch.autograd.Function):
     def backward(ctx, *grads):
         positions, steps = ctx.saved_tensors
         axes, interleaved, magnitude = ctx.how
-        grads = [g if g.stride(2) == 1 else g.contiguous() for g in grads]
+        grads = [g if _beside(g) else g.contiguous() for g in grads]
         return (None, None, None, None, None, *rotary(grads, positions, steps, axes, interleaved, magnitude, inverse=True))
 
 
@@ -221,7 +226,7 @@ class GpuCache:
         return B.mdcnn_cache_desc(*self._desc, table.data_ptr(), n, table.shape[1])
 
     def _side(self, name, t):
-        _need(t.dim() == 3 and t.shape[1] == self.heads and t.shape[2] == self.dim and t.stride(2) == 1, f"{name}: [tokens, {self.heads}, {self.dim}], channels side by side")
+        _need(t.dim() == 3 and t.shape[1] == self.heads and t.shape[2] == self.dim and _beside(t), f"{name}: [tokens, {self.heads}, {self.dim}], channels side by side")
         return B.mdcnn_heads(t.data_ptr(), t.data_ptr(), self.heads, t.stride(0), t.stride(1), t.stride(0), t.stride(1))
 
     def store(self, k, v, table, starts, held, max_new):
@@ -242,3 +247,29 @@ class GpuCache:
             if tokens:
                 B.mdcnn_cache_read(c, self._side("k", k), self._side("v", v), k.shape[0], starts.data_ptr(), first.data_ptr(), max_new, _DTYPE[dtype], _stream(self.device))
         return k, v
+
+    def attend(self, q, table, starts, lengths, max_new, max_len, scale=None, causal=False, window=0, mask=None, out=None):
+        """Attention of queries [tokens, q_heads, dim] (q_heads a multiple of heads) over the cache: sequence s has the queries starts[s] ..
+        starts[s + 1] - 1 and lengths[s] tokens in the cache; max_new and max_len are bounds on both.  scale: of the logits, dim ** -0.5 if not given.
+        causal: the queries are the last tokens of their sequence and see nothing behind themselves, with window > 0 only the `window`
+        tokens up to themselves.  mask: uint8 or bool [sequences, >= max_len], zero: token hidden.  Returns (out, lse): [tokens, q_heads,
+        dim] in the type of q and the natural logarithms of the sums [tokens, q_heads] in float32; zeros and -inf where a query sees nothing."""
+        _need(q.dtype in _DTYPE and q.dim() == 3 and q.shape[2] == self.dim and _beside(q), f"q: [tokens, q_heads, {self.dim}] float32, float16 or bfloat16, channels side by side")
+        tokens, heads, _ = q.shape
+        c = self._cache(table, starts=starts, lengths=lengths)
+        if out is None:
+            out = torch.empty((tokens, heads, self.dim), dtype=q.dtype, device=self.device)
+        _need(out.shape == q.shape and out.dtype == q.dtype and _beside(out), "out: as q")
+        _on(self.device, q=q, out=out, mask=mask)
+        how = B.mdcnn_attend_desc(starts.data_ptr(), lengths.data_ptr(), tokens, max_new, max_len, self.dim ** -0.5 if scale is None else scale, causal, window)
+        if mask is not None:
+            _need(mask.dtype in (torch.uint8, torch.bool) and mask.dim() == 2 and mask.shape[0] == table.shape[0] and mask.shape[1] >= max_len and mask.stride(1) == 1 and mask.stride(0) >= max_len,
+                  f"mask: uint8 or bool [{table.shape[0]}, {max_len} or more]")
+            how.mask_dev, how.mask_row = mask.data_ptr(), mask.stride(0)
+        n = B.mdcnn_cache_attend_bytes(c, how, heads)
+        work = _work(n, self.device)
+        lse = torch.empty((tokens, heads), dtype=torch.float32, device=self.device)
+        side = B.mdcnn_heads(q.data_ptr(), out.data_ptr(), heads, q.stride(0), q.stride(1), out.stride(0), out.stride(1))
+        with torch.cuda.device(self.device):
+            B.mdcnn_cache_attend(c, how, side, _DTYPE[q.dtype], lse.data_ptr(), _ptr(work), n, _stream(self.device))
+        return out, lse

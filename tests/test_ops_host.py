@@ -122,3 +122,31 @@ def test_cache_arguments(call, change, status):
     kw = dict(dtype=1, max_new=100, tokens=200, starts=FAKE, at=FAKE)
     kw.update({k: v for k, v in change.items() if k not in ("c", "k", "v")})
     refused(status, call, cache(**change.get("c", {})), heads(**change.get("k", {})), heads(**change.get("v", {})), kw["tokens"], kw["starts"], kw["at"], kw["max_new"], kw["dtype"])
+
+
+def attending(**kw):
+    a = B.mdcnn_attend_desc(FAKE, FAKE, 6, 2, 300, 0.125, 1, 0, None, 0)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(c=dict(dim=12)), 2), (dict(c=dict(k_dev=None)), 1), (dict(a=dict(tokens=-1)), 2), (dict(a=dict(max_new=-1)), 2), (dict(a=dict(max_len=-1)), 2), (dict(a=dict(causal=2)), 2),
+    (dict(a=dict(window=-1)), 2), (dict(a=dict(window=3, causal=0)), 2), (dict(a=dict(scale=float("inf"))), 2), (dict(a=dict(starts_dev=None)), 1),
+    (dict(a=dict(lengths_dev=FAKE + 2)), 4), (dict(a=dict(mask_dev=FAKE, mask_row=299)), 5), (dict(q=dict(heads=6)), 2), (dict(q=dict(heads=0)), 2), (dict(q=dict(x_dev=None)), 1),
+    (dict(q=dict(y_dev=None)), 1), (dict(q=dict(y_dev=FAKE + 1)), 4), (dict(q=dict(y_token=100)), 2), (dict(dtype=9), 3), (dict(lse=FAKE + 2), 4), (dict(work=FAKE + 8), 4), (dict(n=0), 5),
+    (dict(work=None), 1), (dict(c=dict(n_seq=1 << 20), a=dict(tokens=1 << 30, max_new=1 << 30)), 5)])
+def test_attend_arguments(change, status):
+    big = dict(max_len=100000)
+    big.update(change.get("a", {}))
+    c, a, q = cache(max_pages=2000, **change.get("c", {})), attending(**big), heads(heads=8, x_token=256, y_token=256)
+    for k, v in change.get("q", {}).items():
+        setattr(q, k, v)
+    refused(status, B.mdcnn_cache_attend, c, a, q, change.get("dtype", 1), change.get("lse", FAKE), change.get("work", FAKE), change.get("n", 1 << 40))
+
+
+def test_attend_workspace():
+    c, a = cache(max_pages=2000), attending(max_len=100000)
+    assert B.mdcnn_cache_attend_bytes(c, a, 8) > 0 and B.mdcnn_cache_attend_bytes(c, attending(max_len=100), 8) == 0
+    refused(2, B.mdcnn_cache_attend_bytes, c, a, 6)
