@@ -2,9 +2,15 @@
 keys and values in 8 bits and the attention that reads it.
 
 Argument marshalling only: shapes, strides and types are taken from the tensors, outputs and workspaces come from torch, the
-work is enqueued on the current stream of the tensors' device.  `group_norm_act` is the same for autograd.
+work is enqueued on the current stream of the tensors' device.  `group_norm_act` and `rotary_turn` are the same for autograd.
+
+A call on a small map is as long as its way through the host, so what follows from shapes, strides and types alone - the checks, the description
+for the library, the size of the workspace - is worked out once for each combination (the cached `_.._plan` functions); pointers are
+filled into a copy.
 """
 from __future__ import annotations
+
+import functools
 
 import torch
 
@@ -12,10 +18,7 @@ from . import binding as B
 
 _DTYPE = {torch.float32: B.MDCNN_F32, torch.float16: B.MDCNN_F16, torch.bfloat16: B.MDCNN_BF16}
 _ACT = {"none": B.MDCNN_ACT_NONE, "relu": B.MDCNN_ACT_RELU, "silu": B.MDCNN_ACT_SILU}
-
-
-def _stream(dev):
-    return torch.cuda.current_stream(dev).cuda_stream
+_PLANS = 512                                             # combinations of shapes that are remembered
 
 
 def _need(ok, text):
@@ -23,46 +26,61 @@ def _need(ok, text):
         raise ValueError(text)
 
 
-def _on(dev, **tensors):
-    """Every given tensor is on the GPU `dev`: a pointer of another device would be read there."""
+def _refuse_devices(dev, **tensors):
     _need(dev.type == "cuda", "mdcnn needs GPU tensors: there is no CPU path")
     for name, t in tensors.items():
         _need(t is None or t.device == dev, f"{name} is on {None if t is None else t.device}, not on {dev}")
+
+
+def _on(dev, *tensors):
+    """Whether every given tensor is on the GPU `dev`: a pointer of another device would be read there."""
+    return dev.type == "cuda" and all([t is None or t.device == dev for t in tensors])
 
 
 def _floats(name, t, n):
     _need(t is None or (t.dtype == torch.float32 and t.numel() == n and t.is_contiguous()), f"{name}: {n} contiguous float32 values")
 
 
-def _beside(t):
+def _beside(shape, stride):
     """The last extent's elements lie side by side."""
-    return t.stride(-1) == 1 or t.shape[-1] == 1 or t.numel() == 0
+    return stride[-1] == 1 or shape[-1] == 1 or 0 in shape
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _work(nbytes, dev):
-    return torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+def _like(t):
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+
+def _call(call, dev, *args):
+    """call(*args, stream) with `dev` as the current device and its current stream."""
+    index = dev.index
+    if index == torch.cuda.current_device():
+        call(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(index):
+            call(*args, torch._C._cuda_getCurrentRawStream(index))
 
 
 # -- group norm -----------------------------------------------------------------------------------------------------------
-def _map(name, t, like=None):
-    _need(t.dim() == 4 and (like is None or t.shape == like.shape), f"{name}: a map [N, H, W, C]" + ("" if like is None else f" of shape {tuple(like.shape)}"))
-    _need(t.dtype in _DTYPE and (like is None or t.dtype == like.dtype), f"{name}: float32, float16 or bfloat16" + ("" if like is None else ", as x"))
-    _need(_beside(t), f"{name}: channels last")
-    return B.mdcnn_strides(t.stride(0), t.stride(1), t.stride(2))
+def _strides(name, shape, stride, like):
+    _need(len(shape) == 4 and shape == like, f"{name}: a map [N, H, W, C]" + ("" if shape is like else f" of shape {tuple(like)}"))
+    _need(_beside(shape, stride), f"{name}: channels last")
+    return B.mdcnn_strides(*stride[:3])
 
 
-def _norm_desc(x, groups, gamma, beta, eps, act):
+@functools.lru_cache(_PLANS)
+def _norm_plan(shape, dtype, groups, act, eps, x_stride, y_stride, d_stride=None, backward=False):
+    """(description without pointers, bytes of workspace)"""
+    _need(dtype in _DTYPE, "x: float32, float16 or bfloat16")
     _need(act in _ACT, f"act: one of {', '.join(_ACT)}")
-    xs = _map("x", x)
-    N, H, W, C = x.shape
-    _on(x.device, gamma=gamma, beta=beta)
-    _floats("gamma", gamma, C)
-    _floats("beta", beta, C)
-    return B.mdcnn_group_norm_desc(N, H, W, C, int(groups), _DTYPE[x.dtype], _ACT[act], eps, _ptr(gamma), _ptr(beta), xs, xs, xs)
+    xs = _strides("x", shape, x_stride, shape)
+    ys = _strides("dx" if backward else "out", shape, y_stride, shape)
+    ds = _strides("dy", shape, d_stride, shape) if backward else xs
+    d = B.mdcnn_group_norm_desc(*shape, groups, _DTYPE[dtype], _ACT[act], eps, None, None, xs, ys, ds)
+    return d, B.mdcnn_group_norm_bytes(d, backward)
 
 
 def group_norm(x, groups, gamma=None, beta=None, eps=1e-5, act="none", out=None):
@@ -70,35 +88,44 @@ def group_norm(x, groups, gamma=None, beta=None, eps=1e-5, act="none", out=None)
 
     x may be a view with any strides as long as its channels lie side by side.  Returns (y, mean, rstd), the statistics
     [N, groups] in float32."""
-    d = _norm_desc(x, groups, gamma, beta, eps, act)
+    dev, shape, dtype = x.device, x.shape, x.dtype
+    if not _on(dev, gamma, beta, out):
+        _refuse_devices(dev, gamma=gamma, beta=beta, out=out)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _on(x.device, out=out)
-    d.ys = _map("out", out, x)
-    n = B.mdcnn_group_norm_bytes(d)
-    stats = torch.empty((2, x.shape[0], int(groups)), dtype=torch.float32, device=x.device)
-    work = _work(n, x.device)
-    with torch.cuda.device(x.device):
-        B.mdcnn_group_norm(d, x.data_ptr(), out.data_ptr(), stats[0].data_ptr(), stats[1].data_ptr(), _ptr(work), n, _stream(x.device))
-    return out, stats[0], stats[1]
+        out = _like(x)
+    else:
+        _need(out.shape == shape and out.dtype == dtype, "out: as x")
+    plan, n = _norm_plan(shape, dtype, groups, act, eps, x.stride(), out.stride())
+    _floats("gamma", gamma, shape[3])
+    _floats("beta", beta, shape[3])
+    d = B.mdcnn_group_norm_desc.from_buffer_copy(plan)
+    d.gamma_dev, d.beta_dev = _ptr(gamma), _ptr(beta)
+    mean = torch.empty((shape[0], groups), dtype=torch.float32, device=dev)
+    rstd = torch.empty_like(mean)
+    work = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    _call(B.mdcnn_group_norm, dev, d, x.data_ptr(), out.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _ptr(work), n)
+    return out, mean, rstd
 
 
 def group_norm_backward(x, dy, mean, rstd, groups, gamma=None, beta=None, act="none"):
     """Gradients (dx, dgamma, dbeta) of group_norm from the gradient dy of y and the statistics it returned."""
-    d = _norm_desc(x, groups, gamma, beta, 0.0, act)
-    _on(x.device, dy=dy, mean=mean, rstd=rstd)
-    d.ds = _map("dy", dy, x)
-    _floats("mean", mean, x.shape[0] * int(groups))
-    _floats("rstd", rstd, x.shape[0] * int(groups))
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    d.ys = _map("dx", dx, x)
-    n = B.mdcnn_group_norm_bytes(d, True)
-    grads = torch.empty((2, x.shape[3]), dtype=torch.float32, device=x.device)
-    work = _work(n, x.device)
-    with torch.cuda.device(x.device):
-        B.mdcnn_group_norm_backward(d, x.data_ptr(), dy.data_ptr(), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), grads[0].data_ptr(), grads[1].data_ptr(),
-                                    _ptr(work), n, _stream(x.device))
-    return dx, grads[0], grads[1]
+    dev, shape, dtype = x.device, x.shape, x.dtype
+    if not _on(dev, dy, mean, rstd, gamma, beta):
+        _refuse_devices(dev, dy=dy, mean=mean, rstd=rstd, gamma=gamma, beta=beta)
+    _need(dy.shape == shape and dy.dtype == dtype, "dy: as x")
+    dx = _like(x)
+    plan, n = _norm_plan(shape, dtype, groups, act, 0.0, x.stride(), dx.stride(), dy.stride(), True)
+    _floats("gamma", gamma, shape[3])
+    _floats("beta", beta, shape[3])
+    _floats("mean", mean, shape[0] * groups)
+    _floats("rstd", rstd, shape[0] * groups)
+    d = B.mdcnn_group_norm_desc.from_buffer_copy(plan)
+    d.gamma_dev, d.beta_dev = _ptr(gamma), _ptr(beta)
+    dgamma = torch.empty(shape[3], dtype=torch.float32, device=dev)
+    dbeta = torch.empty_like(dgamma)
+    work = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    _call(B.mdcnn_group_norm_backward, dev, d, x.data_ptr(), dy.data_ptr(), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), _ptr(work), n)
+    return dx, dgamma, dbeta
 
 
 class _GroupNormAct(torch.autograd.Function):
@@ -113,7 +140,7 @@ class _GroupNormAct(torch.autograd.Function):
     def backward(ctx, dy):
         x, gamma, beta, mean, rstd = ctx.saved_tensors
         groups, act = ctx.how
-        if not _beside(dy):
+        if not _beside(dy.shape, dy.stride()):
             dy = dy.contiguous()
         dx, dgamma, dbeta = group_norm_backward(x, dy, mean, rstd, groups, gamma, beta, act)
         return dx, None, None if gamma is None else dgamma, None if beta is None else dbeta, None, None
@@ -139,10 +166,17 @@ def rotary_steps(turned, axes=1, base=10000.0, scaling="none", factor=1.0, origi
     return torch.tensor([n - (1 << 64) if n >= 1 << 63 else n for n in steps], dtype=torch.int64, device=device)
 
 
-def _heads(name, t, dtype, dim, tokens):
-    _need(t.dim() == 3 and t.shape[0] == tokens and t.shape[2] == dim, f"{name}: [{tokens}, heads, {dim}]")
-    _need(t.dtype == dtype, f"{name}: {dtype}")
-    _need(_beside(t), f"{name}: channels side by side")
+@functools.lru_cache(_PLANS)
+def _heads_plan(name, like, x_shape, x_stride, y_shape, y_stride):
+    _need(len(x_shape) == 3 and x_shape[0] == like[0] and x_shape[2] == like[2] and _beside(x_shape, x_stride), f"{name}: [{like[0]}, heads, {like[2]}], channels side by side")
+    _need(y_shape == x_shape and _beside(y_shape, y_stride), f"the output of {name}: of its shape, channels side by side")
+    return B.mdcnn_heads(None, None, x_shape[1], x_stride[0], x_stride[1], y_stride[0], y_stride[1])
+
+
+def _heads(name, x, y, like):
+    h = B.mdcnn_heads.from_buffer_copy(_heads_plan(name, like, x.shape, x.stride(), y.shape, y.stride()))
+    h.x_dev, h.y_dev = x.data_ptr(), y.data_ptr()
+    return h
 
 
 def rotary(maps, positions, steps, axes=1, interleaved=False, magnitude=1.0, inverse=False, out=None):
@@ -150,24 +184,17 @@ def rotary(maps, positions, steps, axes=1, interleaved=False, magnitude=1.0, inv
     side) by positions [tokens] or [tokens, axes] int32; the others are copied.  Returns new tensors, or `out` (which may be `maps`
     themselves).  inverse=True turns back by the same angles, times magnitude: the gradient."""
     first = maps[0]
-    tokens, dim, dev = first.shape[0], first.shape[-1], first.device
-    _need(1 <= len(maps) <= 2, "maps: one or two")
-    _need(first.dtype in _DTYPE, "maps: float32, float16 or bfloat16")
-    _need(positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == tokens * axes, f"positions: {tokens} x {axes} contiguous int32 values")
+    shape, dev, dtype = first.shape, first.device, first.dtype
+    _need(1 <= len(maps) <= 2 and (out is None or len(out) == len(maps)), "maps: one or two, out: as many")
+    out = [_like(m) for m in maps] if out is None else list(out)
+    if not _on(dev, positions, steps, *maps, *out):
+        _refuse_devices(dev, positions=positions, steps=steps, **{f"maps[{i}]": m for i, m in enumerate(maps)}, **{f"out[{i}]": m for i, m in enumerate(out)})
+    _need(dtype in _DTYPE and all([m.dtype == dtype for m in (*maps, *out)]), "maps and out: float32, float16 or bfloat16, all of one type")
+    hs = [_heads("the first map" if i == 0 else "the second map", x, y, shape) for i, (x, y) in enumerate(zip(maps, out))]
+    _need(positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == shape[0] * axes, f"positions: {shape[0]} x {axes} contiguous int32 values")
     _need(steps.dtype == torch.int64 and steps.dim() == 1 and steps.is_contiguous(), "steps: contiguous int64 values of rotary_steps")
-    if out is None:
-        out = [torch.empty(m.shape, dtype=m.dtype, device=dev) for m in maps]
-    _on(dev, positions=positions, steps=steps, **{f"maps[{i}]": m for i, m in enumerate(maps)}, **{f"out[{i}]": m for i, m in enumerate(out)})
-    _need(len(out) == len(maps), "out: one tensor for each map")
-    hs = []
-    for i, (x, y) in enumerate(zip(maps, out)):
-        _heads(f"maps[{i}]", x, first.dtype, dim, tokens)
-        _heads(f"out[{i}]", y, first.dtype, dim, tokens)
-        _need(x.shape[1] == y.shape[1], "out: as many heads as maps")
-        hs.append(B.mdcnn_heads(x.data_ptr(), y.data_ptr(), x.shape[1], x.stride(0), x.stride(1), y.stride(0), y.stride(1)))
-    with torch.cuda.device(dev):
-        B.mdcnn_rotary(hs, tokens, dim, _DTYPE[first.dtype], positions.data_ptr(), axes, steps.data_ptr(), 2 * steps.numel(), interleaved, inverse, magnitude, _stream(dev))
-    return list(out)
+    _call(B.mdcnn_rotary, dev, hs, shape[0], shape[2], _DTYPE[dtype], positions.data_ptr(), axes, steps.data_ptr(), 2 * steps.numel(), interleaved, inverse, magnitude)
+    return out
 
 
 class _Rotary(torch.autograd.Function):
@@ -181,7 +208,7 @@ class _Rotary(torch.autograd.Function):
     def backward(ctx, *grads):
         positions, steps = ctx.saved_tensors
         axes, interleaved, magnitude = ctx.how
-        grads = [g if _beside(g) else g.contiguous() for g in grads]
+        grads = [g if _beside(g.shape, g.stride()) else g.contiguous() for g in grads]
         return (None, None, None, None, None, *rotary(grads, positions, steps, axes, interleaved, magnitude, inverse=True))
 
 
@@ -191,6 +218,10 @@ def rotary_turn(maps, positions, steps, axes=1, interleaved=False, magnitude=1.0
 
 
 # -- the cache --------------------------------------------------------------------------------------------------------------
+def _per_sequence(name, t, n):
+    _need(t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n, f"{name}: {n} contiguous int32 values")
+
+
 class GpuCache:
     """Keys and values in pages of 64 tokens, 8 bits a value with one scale for each page and head.
 
@@ -205,9 +236,9 @@ class GpuCache:
         _need(k.dtype == v.dtype == torch.int8 and k.shape == (pages, heads, 64, pitch) and v.shape == (pages, heads, pitch, 64), f"k, v: int8 [pages, heads, 64, {pitch}] and [pages, heads, {pitch}, 64]")
         _need(k_scale.dtype == v_scale.dtype == torch.float32 and k_scale.shape == v_scale.shape == (pages, heads), "k_scale, v_scale: float32 [pages, heads]")
         _need(all(t.is_contiguous() for t in (k, v, k_scale, v_scale)), "k, v, k_scale, v_scale: contiguous")
-        _on(dev, v=v, k_scale=k_scale, v_scale=v_scale)
+        _refuse_devices(dev, v=v, k_scale=k_scale, v_scale=v_scale)
         self.k, self.v, self.k_scale, self.v_scale, self.dim, self.heads, self.device = k, v, k_scale, v_scale, int(dim), heads, dev
-        self._desc = (pages, heads, int(dim), k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+        self._plan = B.mdcnn_cache_desc(pages, heads, int(dim), k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), None, 0, 0)
 
     @classmethod
     def empty(cls, pages, heads, dim, device="cuda:0"):
@@ -217,35 +248,38 @@ class GpuCache:
         scales = torch.empty((2, pages, heads), dtype=torch.float32, device=device)
         return cls(codes[0].view(pages, heads, 64, pitch), codes[1].view(pages, heads, pitch, 64), scales[0], scales[1], dim)
 
-    def _cache(self, table, **per_sequence):
+    def _cache(self, table):
         _need(table.dtype == torch.int32 and table.dim() == 2 and table.is_contiguous(), "table: contiguous int32 [sequences, max_pages]")
-        n = table.shape[0]
-        for name, t in per_sequence.items():
-            _need(t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n + (name == "starts"), f"{name}: {n + (name == 'starts')} contiguous int32 values")
-        _on(self.device, table=table, **per_sequence)
-        return B.mdcnn_cache_desc(*self._desc, table.data_ptr(), n, table.shape[1])
-
-    def _side(self, name, t):
-        _need(t.dim() == 3 and t.shape[1] == self.heads and t.shape[2] == self.dim and _beside(t), f"{name}: [tokens, {self.heads}, {self.dim}], channels side by side")
-        return B.mdcnn_heads(t.data_ptr(), t.data_ptr(), self.heads, t.stride(0), t.stride(1), t.stride(0), t.stride(1))
+        c = B.mdcnn_cache_desc.from_buffer_copy(self._plan)
+        c.table_dev = table.data_ptr()
+        c.n_seq, c.max_pages = table.shape
+        return c
 
     def store(self, k, v, table, starts, held, max_new):
         """Puts new tokens [tokens, heads, dim] into their pages: sequence s has tokens starts[s] .. starts[s + 1] - 1, which follow the held[s]
         that it has already.  max_new: no sequence has more new tokens."""
-        _need(k.dtype == v.dtype and k.dtype in _DTYPE and k.shape == v.shape, "k, v: float32, float16 or bfloat16 of one shape")
-        _on(self.device, k=k, v=v)
-        c = self._cache(table, starts=starts, held=held)
-        with torch.cuda.device(self.device):
-            B.mdcnn_cache_store(c, self._side("k", k), self._side("v", v), k.shape[0], starts.data_ptr(), held.data_ptr(), max_new, _DTYPE[k.dtype], _stream(self.device))
+        dev, shape = self.device, k.shape
+        if not _on(dev, k, v, table, starts, held):
+            _refuse_devices(dev, k=k, v=v, table=table, starts=starts, held=held)
+        _need(k.dtype == v.dtype and k.dtype in _DTYPE and v.shape == shape and len(shape) == 3 and shape[1:] == (self.heads, self.dim),
+              f"k, v: [tokens, {self.heads}, {self.dim}] float32, float16 or bfloat16, of one type")
+        c = self._cache(table)
+        _per_sequence("starts", starts, c.n_seq + 1)
+        _per_sequence("held", held, c.n_seq)
+        _call(B.mdcnn_cache_store, dev, c, _heads("k", k, k, shape), _heads("v", v, v, shape), shape[0], starts.data_ptr(), held.data_ptr(), max_new, _DTYPE[k.dtype])
 
     def read(self, table, starts, first, max_new, tokens, dtype):
         """The values of tokens first[s] .. of every sequence s, starts[s + 1] - starts[s] of them, as (k, v) [tokens, heads, dim]; tokens = starts[-1]."""
+        dev = self.device
+        if not _on(dev, table, starts, first):
+            _refuse_devices(dev, table=table, starts=starts, first=first)
         _need(dtype in _DTYPE, "dtype: float32, float16 or bfloat16")
-        k, v = (torch.empty((tokens, self.heads, self.dim), dtype=dtype, device=self.device) for _ in range(2))
-        c = self._cache(table, starts=starts, first=first)
-        with torch.cuda.device(self.device):
-            if tokens:
-                B.mdcnn_cache_read(c, self._side("k", k), self._side("v", v), k.shape[0], starts.data_ptr(), first.data_ptr(), max_new, _DTYPE[dtype], _stream(self.device))
+        c = self._cache(table)
+        _per_sequence("starts", starts, c.n_seq + 1)
+        _per_sequence("first", first, c.n_seq)
+        k = torch.empty((tokens, self.heads, self.dim), dtype=dtype, device=dev)
+        v = torch.empty_like(k)
+        _call(B.mdcnn_cache_read, dev, c, _heads("k", k, k, k.shape), _heads("v", v, v, k.shape), tokens, starts.data_ptr(), first.data_ptr(), max_new, _DTYPE[dtype])
         return k, v
 
     def attend(self, q, table, starts, lengths, max_new, max_len, scale=None, causal=False, window=0, mask=None, out=None):
@@ -254,22 +288,24 @@ class GpuCache:
         causal: the queries are the last tokens of their sequence and see nothing behind themselves, with window > 0 only the `window`
         tokens up to themselves.  mask: uint8 or bool [sequences, >= max_len], zero: token hidden.  Returns (out, lse): [tokens, q_heads,
         dim] in the type of q and the natural logarithms of the sums [tokens, q_heads] in float32; zeros and -inf where a query sees nothing."""
-        _need(q.dtype in _DTYPE and q.dim() == 3 and q.shape[2] == self.dim and _beside(q), f"q: [tokens, q_heads, {self.dim}] float32, float16 or bfloat16, channels side by side")
-        tokens, heads, _ = q.shape
-        c = self._cache(table, starts=starts, lengths=lengths)
+        dev, shape = self.device, q.shape
+        if not _on(dev, q, table, starts, lengths, mask, out):
+            _refuse_devices(dev, q=q, table=table, starts=starts, lengths=lengths, mask=mask, out=out)
+        _need(q.dtype in _DTYPE and len(shape) == 3 and shape[2] == self.dim, f"q: [tokens, q_heads, {self.dim}] float32, float16 or bfloat16")
         if out is None:
-            out = torch.empty((tokens, heads, self.dim), dtype=q.dtype, device=self.device)
-        _need(out.shape == q.shape and out.dtype == q.dtype and _beside(out), "out: as q")
-        _on(self.device, q=q, out=out, mask=mask)
-        how = B.mdcnn_attend_desc(starts.data_ptr(), lengths.data_ptr(), tokens, max_new, max_len, self.dim ** -0.5 if scale is None else scale, causal, window)
+            out = _like(q)
+        else:
+            _need(out.shape == shape and out.dtype == q.dtype, "out: as q")
+        c = self._cache(table)
+        _per_sequence("starts", starts, c.n_seq + 1)
+        _per_sequence("lengths", lengths, c.n_seq)
+        how = B.mdcnn_attend_desc(starts.data_ptr(), lengths.data_ptr(), shape[0], max_new, max_len, self.dim ** -0.5 if scale is None else scale, causal, window)
         if mask is not None:
-            _need(mask.dtype in (torch.uint8, torch.bool) and mask.dim() == 2 and mask.shape[0] == table.shape[0] and mask.shape[1] >= max_len and mask.stride(1) == 1 and mask.stride(0) >= max_len,
-                  f"mask: uint8 or bool [{table.shape[0]}, {max_len} or more]")
+            _need(mask.dtype in (torch.uint8, torch.bool) and mask.dim() == 2 and mask.shape[0] == c.n_seq and mask.shape[1] >= max_len and mask.stride(1) == 1 and mask.stride(0) >= max_len,
+                  f"mask: uint8 or bool [{c.n_seq}, {max_len} or more]")
             how.mask_dev, how.mask_row = mask.data_ptr(), mask.stride(0)
-        n = B.mdcnn_cache_attend_bytes(c, how, heads)
-        work = _work(n, self.device)
-        lse = torch.empty((tokens, heads), dtype=torch.float32, device=self.device)
-        side = B.mdcnn_heads(q.data_ptr(), out.data_ptr(), heads, q.stride(0), q.stride(1), out.stride(0), out.stride(1))
-        with torch.cuda.device(self.device):
-            B.mdcnn_cache_attend(c, how, side, _DTYPE[q.dtype], lse.data_ptr(), _ptr(work), n, _stream(self.device))
+        n = B.mdcnn_cache_attend_bytes(c, how, shape[1])
+        work = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+        lse = torch.empty(shape[:2], dtype=torch.float32, device=dev)
+        _call(B.mdcnn_cache_attend, dev, c, how, _heads("q", q, out, shape), _DTYPE[q.dtype], lse.data_ptr(), _ptr(work), n)
         return out, lse
