@@ -687,7 +687,7 @@ typedef struct {
     int pages, heads, dim;    /* 1 <= heads, 8 <= dim <= 256, a multiple of 8           */
     int8_t* k_dev;            /* pages * heads * 64 * pitch bytes each, 16-byte aligned */
     int8_t* v_dev;
-    float* k_scale_dev;       /* pages * heads                                          */
+    float* k_scale_dev;       /* pages * heads, none negative                           */
     float* v_scale_dev;
     const int* table_dev;     /* n_seq * max_pages page numbers; entries outside 0 .. pages - 1 hold no page */
     int n_seq, max_pages;
@@ -727,8 +727,9 @@ typedef struct {
     const uint8_t* mask_dev;  /* n_seq rows of mask_row bytes, byte j: token j; or NULL  */
     long long mask_row;       /* >= max_len                                             */
 } mdcnn_attend_desc;
+/* Workspace of the call, in bytes (may be 0). */
 mdcnn_status mdcnn_cache_attend_bytes(const mdcnn_cache_desc* c, const mdcnn_attend_desc* a, int q_heads,
-                                      size_t* bytes);
+                                      int dtype, size_t* bytes);
 /* q: queries and output (x and y), dtype f32, f16 or bf16; lse_dev: tokens * q->heads floats, natural logarithm, or NULL. */
 mdcnn_status mdcnn_cache_attend(const mdcnn_cache_desc* c, const mdcnn_attend_desc* a, const mdcnn_heads* q,
                                 int dtype, float* lse_dev, void* work_dev, size_t work_bytes, void* stream);

@@ -146,7 +146,7 @@ def lib():
         hs, cd = C.POINTER(mdcnn_heads), C.POINTER(mdcnn_cache_desc)
         L.mdcnn_cache_store.argtypes = [cd, hs, hs, C.c_int, vp, vp, C.c_int, C.c_int, vp]
         L.mdcnn_cache_read.argtypes = [cd, hs, hs, C.c_int, vp, vp, C.c_int, C.c_int, vp]
-        L.mdcnn_cache_attend_bytes.argtypes = [cd, C.POINTER(mdcnn_attend_desc), C.c_int, C.POINTER(sz)]
+        L.mdcnn_cache_attend_bytes.argtypes = [cd, C.POINTER(mdcnn_attend_desc), C.c_int, C.c_int, C.POINTER(sz)]
         L.mdcnn_cache_attend.argtypes = [cd, C.POINTER(mdcnn_attend_desc), hs, C.c_int, vp, vp, sz, vp]
         L.mdcnn_last_error.restype = C.c_char_p
         L.mdcnn_version.restype = C.c_char_p
@@ -468,9 +468,9 @@ def mdcnn_cache_read(cache: mdcnn_cache_desc, k: mdcnn_heads, v: mdcnn_heads, to
     _check(lib().mdcnn_cache_read(C.byref(cache), C.byref(k), C.byref(v), tokens, starts_ptr, first_ptr, max_new, dtype, stream))
 
 
-def mdcnn_cache_attend_bytes(cache: mdcnn_cache_desc, how: mdcnn_attend_desc, q_heads: int) -> int:
+def mdcnn_cache_attend_bytes(cache: mdcnn_cache_desc, how: mdcnn_attend_desc, q_heads: int, dtype: int) -> int:
     n = C.c_size_t()
-    _check(lib().mdcnn_cache_attend_bytes(C.byref(cache), C.byref(how), q_heads, C.byref(n)))
+    _check(lib().mdcnn_cache_attend_bytes(C.byref(cache), C.byref(how), q_heads, dtype, C.byref(n)))
     return n.value
 
 

@@ -7,8 +7,11 @@
 // neighbouring tokens, which is how the values lie in a page.
 //
 // Codes become halves without a conversion: a byte c + 128 in the low byte of 0x6400 is the half 1152 + c, minus 1152 is c,
-// exactly.  Scales are multiplied in where the sums are: that of the keys with the logits, that of the values with the probabilities,
-// relative to the largest one so far (so that halves hold them whatever their size).
+// exactly.  The scale of a page's keys is multiplied into the logits.  That of its values goes into the exponent,
+//   w = 2^(x + log2 vs - T),  T the row's largest x + log2 vs so far,
+// so that w is a half of full precision next to what counts most in this row, whatever the sizes of scales and values: sum w code / sum (w / vs)
+// is the result, 2^T sum (w / vs) the sum of the exponentials.  A page whose values are all zeros (vs below 2^-100) takes the scale of the
+// one before and weights of zero in the first sum.  (Scales of one sequence and head may lie 2^100 apart.)
 #pragma once
 
 #include "ops_device.h"
@@ -59,6 +62,41 @@ struct Rows {
     __device__ __forceinline__ int lo(const AttendJob& j, int i) const { return j.window ? max(0, len - n + i + 1 - j.window) : 0; }
 };
 
+// Pages of the rows r0 .. r1 - 1 of a sequence, of which split z has the run [first, last).
+struct Run {
+    int first, last, splits;
+    __device__ __forceinline__ Run(const AttendJob& j, const Rows& s, int r0, int r1, int z) {
+        const int lo = s.lo(j, r0 / j.group), hi = s.hi(j, (r1 - 1) / j.group);
+        const int p0 = lo / MDCNN_PAGE_TOKENS, p1 = min((hi + MDCNN_PAGE_TOKENS - 1) / MDCNN_PAGE_TOKENS, j.max_pages);
+        splits = max(0, (p1 - p0 + j.run - 1) / j.run);
+        first = p0 + z * j.run;
+        last = min(p1, first + j.run);
+    }
+};
+
+// The scale of a page's values in the exponent.  Its logarithm is rounded to 32 bits, which takes up to 2^-21 of the values; the inverse is that of the
+// rounded one, so that the sum of the exponentials does not notice.
+struct ValueScale {
+    float log = 0.f, inverse = 1.f;
+    bool none = false, bad = false;                        // weights do not count in the sum of values; not a number
+    __device__ __forceinline__ void next(float vs) {
+        bad = vs != vs;
+        none = vs < 7.8886090522101181e-31f;               // 2^-100; any scale does then: that of the page before
+        if (!none && !bad) {
+            log = __builtin_amdgcn_logf(vs);
+            inverse = exp2_fast(-log);
+        }
+    }
+};
+
+// Factor of the products of a row with a page's keys.  Never zero: a hidden token's minus infinity stays that.
+__device__ __forceinline__ float factor_of(float logit, float ks) {
+    const float by = logit * ks;
+    return by < 1e-30f ? 1e-30f : by;
+}
+// How far a weight may lie above one before its row's T is moved (weights are halves): sums are rescaled on few pages only.
+constexpr float kSlack = 8.f;
+
 // The power of two that brings the largest magnitude of a row to 2^13 .. 2^14 (1 for none, or one that is not finite).
 __device__ __forceinline__ int exponent_of(float top) {
     const int e = (int)(__float_as_uint(top) >> 23);
@@ -80,6 +118,25 @@ __device__ __forceinline__ unsigned mask_bits(const uint8_t* row, int pos, int e
             if (pos + i < end && row[pos + i]) bits |= 1u << i;
     }
     return bits;
+}
+
+// What::go<storage type, pitch>(j, st)
+template <typename What, typename T>
+hipError_t for_pitch(const AttendJob& j, hipStream_t st) {
+    switch (j.pitch) {
+        case 32: return What::template go<T, 32>(j, st);
+        case 64: return What::template go<T, 64>(j, st);
+        case 96: return What::template go<T, 96>(j, st);
+        case 128: return What::template go<T, 128>(j, st);
+        case 192: return What::template go<T, 192>(j, st);
+        default: return What::template go<T, 256>(j, st);
+    }
+}
+template <typename What>
+hipError_t for_type_and_pitch(const AttendJob& j, int dtype, hipStream_t st) {
+    if (dtype == MDCNN_F32) return for_pitch<What, float>(j, st);
+    if (dtype == MDCNN_F16) return for_pitch<What, _Float16>(j, st);
+    return for_pitch<What, __bf16>(j, st);
 }
 
 }  // namespace mdcnn

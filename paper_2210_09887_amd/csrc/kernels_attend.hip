@@ -27,18 +27,6 @@ struct AttendBlock {
     }
 };
 
-// Pages of a block: those of the rows r0 .. r1 - 1, of which split z has the run [first, last).
-struct Run {
-    int first, last, splits;
-    __device__ __forceinline__ Run(const AttendJob& j, const Rows& s, int r0, int r1, int z) {
-        const int lo = s.lo(j, r0 / j.group), hi = s.hi(j, (r1 - 1) / j.group);
-        const int p0 = lo / kPage, p1 = min((hi + kPage - 1) / kPage, j.max_pages);
-        splits = max(0, (p1 - p0 + j.run - 1) / j.run);
-        first = p0 + z * j.run;
-        last = min(p1, first + j.run);
-    }
-};
-
 template <typename T, int DP>
 __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(AttendJob j) {
     constexpr bool kTwo = sizeof(T) == 4;                  // fp32 queries and probabilities as sums of two halves
@@ -79,17 +67,18 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
         for (int st = 0; st < NS; ++st)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float x = scaled(f[st][i], -e);
+                const float x = scaled(j.scale < 0.f ? -f[st][i] : f[st][i], -e);
                 qh[st][i] = (_Float16)x;
                 if constexpr (kTwo) ql[st][i] = (_Float16)(x - (float)qh[st][i]);
             }
     }
-    const float logit = scaled(j.scale * kLog2E, e);
+    const float logit = scaled(fabsf(j.scale) * kLog2E, e);      // (the queries have its sign)
     const int hi = live ? s.hi(j, query) : 0, lo = live ? s.lo(j, query) : 0;
     const int all_hi = s.hi(j, r0 / j.group), all_lo = s.lo(j, (r1 - 1) / j.group);      // seen by every row
     const uint8_t* mask = j.mask ? j.mask + seq * j.mask_row : nullptr;
 
-    float top = -INFINITY, sum = 0.f, ref = 0.f;           // maximum and sum of this lane's row, largest scale of the values
+    float top = -INFINITY, sum = 0.f;                      // T and sum of this lane's row
+    ValueScale val;
     float4v out[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) out[v] = float4v{0.f, 0.f, 0.f, 0.f};
@@ -148,11 +137,11 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
             __builtin_amdgcn_sched_barrier(0);             // or all codes are made halves first, in as many registers
         }
         load_keys(next);
-        // logits in powers of two; hidden ones minus infinity
-        const float by = logit * ks;
+        const float by = factor_of(logit, ks);
+        val.next(vs);
         float x[16];
 #pragma unroll
-        for (int t = 0; t < 16; ++t) x[t] = acc[t / 4][t % 4] * by;
+        for (int t = 0; t < 16; ++t) x[t] = acc[t / 4][t % 4];
         unsigned seen = 0xffffu;
         const int pos = p * kPage + 16 * quad;
         if (p * kPage < all_lo || (p + 1) * kPage > all_hi || mask) {
@@ -168,34 +157,29 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
         for (int t = 1; t < 16; ++t) m = fmaxf(m, x[t]);
         m = fmaxf(m, __shfl_xor(m, 16, 64));
         m = fmaxf(m, __shfl_xor(m, 32, 64));
-        m = fmaxf(m, top);
-        const float base = m == -INFINITY ? 0.f : m;       // (nothing seen so far: all probabilities come out as zeros)
-        const float fade = exp2_fast(top - base);
-        top = m;
-        float fade_out = fade, rel;                        // scale of the values relative to the largest so far
-        if (vs <= ref) {
-            rel = ref > 0.f ? vs / ref : 0.f;
-        } else if (vs == vs) {
-            fade_out *= ref / vs;
-            ref = vs;
-            rel = 1.f;
-        } else {
-            rel = vs;                                      // not a number: the tokens that are seen make the row one
+        m = m * by + val.log;
+        if (__any(m > top + kSlack)) {
+            const float next_top = fmaxf(top, m), fade = next_top == -INFINITY ? 1.f : exp2_fast(top - next_top);
+            top = next_top;
+            sum *= fade;
+#pragma unroll
+            for (int v = 0; v < NV; ++v) out[v] *= fade;
         }
+        const float base = val.log - (top == -INFINITY ? 0.f : top);
         float add = 0.f;
         half8 ph[2], pl[kTwo ? 2 : 1];
 #pragma unroll
         for (int t = 0; t < 16; ++t) {
-            const float w = exp2_fast(x[t] - base);
+            float w = exp2_fast(__builtin_fmaf(x[t], by, base));
+            w = seen >> t & 1 ? w : 0.f;                   // (whatever the scales of a hidden token are)
             add += w;
-            const float y = seen >> t & 1 ? w * rel : 0.f;
-            ph[t / 8][t % 8] = (_Float16)y;
-            if constexpr (kTwo) pl[t / 8][t % 8] = (_Float16)(y - (float)ph[t / 8][t % 8]);
+            w = val.none ? 0.f : val.bad && seen >> t & 1 ? vs : w;
+            ph[t / 8][t % 8] = (_Float16)w;
+            if constexpr (kTwo) pl[t / 8][t % 8] = (_Float16)(w - (float)ph[t / 8][t % 8]);
         }
-        sum = sum * fade + add;
+        sum += add * val.inverse;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            out[v] *= fade_out;
             const half8 a = halves_of(vr[v][0], vr[v][1]), b = halves_of(vr[v][2], vr[v][3]);
             out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, ph[0], out[v], 0, 0, 0);
             out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, ph[1], out[v], 0, 0, 0);
@@ -214,7 +198,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
     sum += __shfl_xor(sum, 32, 64);
     if (quad == 0) { s_top[wave][n] = top; s_sum[wave][n] = sum; }
 #pragma unroll
-    for (int v = 0; v < NV; ++v) *(float4v*)&s_out[wave][n][16 * v + 4 * quad] = out[v] * ref;
+    for (int v = 0; v < NV; ++v) *(float4v*)&s_out[wave][n][16 * v + 4 * quad] = out[v];
     __syncthreads();
     const int m = threadIdx.x / 16, c0 = threadIdx.x % 16;
     if (r0 + m >= s.rows) return;
@@ -254,12 +238,12 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendJob j) {
     const int r = blockIdx.x % per, head = blockIdx.x / per % j.heads, seq = blockIdx.x / per / j.heads;
     Rows s;
     if (!s.load(j, seq) || r >= s.rows) return;
-    const int tile = r / 16, m = r % 16;
-    const Run run(j, s, tile * 16, min(tile * 16 + 16, s.rows), 0);
+    const int tile = r / j.tile_rows, m = r % j.tile_rows;
+    const Run run(j, s, tile * j.tile_rows, min((tile + 1) * j.tile_rows, s.rows), 0);
     if (run.splits <= 1) return;
     const long long slot = (((long long)seq * j.heads + head) * j.tiles + tile) * j.splits;
     float peak = -INFINITY;
-    for (int z = threadIdx.x & 63; z < run.splits; z += 64) peak = fmaxf(peak, j.part_top[(slot + z) * 16 + m].x);
+    for (int z = threadIdx.x & 63; z < run.splits; z += 64) peak = fmaxf(peak, j.part_top[(slot + z) * j.tile_rows + m].x);
 #pragma unroll
     for (int k = 1; k < 64; k <<= 1) peak = fmaxf(peak, __shfl_xor(peak, k, 64));
     const float base = peak == -INFINITY ? 0.f : peak;
@@ -269,10 +253,10 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendJob j) {
         float total = 0.f;
 #pragma unroll 4
         for (int z = set; z < run.splits; z += kSets) {
-            const float2 t = j.part_top[(slot + z) * 16 + m];
+            const float2 t = j.part_top[(slot + z) * j.tile_rows + m];
             const float w = exp2_fast(t.x - base);
             total += w * t.y;
-            x += w * *(const float4v*)(j.part_out + ((slot + z) * 16 + m) * DP + 4 * c);
+            x += w * *(const float4v*)(j.part_out + ((slot + z) * j.tile_rows + m) * DP + 4 * c);
         }
         s_part[set][c] = x;
         if (c == 0) s_sum[set] = total;
@@ -291,29 +275,27 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendJob j) {
 }
 
 template <typename T, int DP>
-hipError_t launch(const AttendJob& j, hipStream_t st) {
-    k_attend_rows<T, DP><<<(unsigned)((long long)j.splits * j.tiles * j.n_seq * j.heads), kThreads, 0, st>>>(j);
+hipError_t launch_join(const AttendJob& j, hipStream_t st) {
     if (j.splits > 1) k_attend_join<T, DP><<<(unsigned)((long long)j.max_new * j.group * j.n_seq * j.heads), kThreads, 0, st>>>(j);
     return hipGetLastError();
 }
-template <typename T>
-hipError_t launch_of(const AttendJob& j, hipStream_t st) {
-    switch (j.pitch) {
-        case 32: return launch<T, 32>(j, st);
-        case 64: return launch<T, 64>(j, st);
-        case 96: return launch<T, 96>(j, st);
-        case 128: return launch<T, 128>(j, st);
-        case 192: return launch<T, 192>(j, st);
-        default: return launch<T, 256>(j, st);
-    }
+template <typename T, int DP>
+hipError_t launch(const AttendJob& j, hipStream_t st) {
+    k_attend_rows<T, DP><<<(unsigned)((long long)j.splits * j.tiles * j.n_seq * j.heads), kThreads, 0, st>>>(j);
+    return hipGetLastError();
 }
+struct Rows16 {
+    template <typename T, int DP>
+    static hipError_t go(const AttendJob& j, hipStream_t st) { return launch<T, DP>(j, st); }
+};
+struct Join {
+    template <typename T, int DP>
+    static hipError_t go(const AttendJob& j, hipStream_t st) { return launch_join<T, DP>(j, st); }
+};
 
 }  // namespace
 
-hipError_t launch_attend_rows(const AttendJob& j, int dtype, hipStream_t st) {
-    if (dtype == MDCNN_F32) return launch_of<float>(j, st);
-    if (dtype == MDCNN_F16) return launch_of<_Float16>(j, st);
-    return launch_of<__bf16>(j, st);
-}
+hipError_t launch_attend_rows(const AttendJob& j, int dtype, hipStream_t st) { return for_type_and_pitch<Rows16>(j, dtype, st); }
+hipError_t launch_attend_join(const AttendJob& j, int dtype, hipStream_t st) { return for_type_and_pitch<Join>(j, dtype, st); }
 
 }  // namespace mdcnn

@@ -1,0 +1,272 @@
+// Attention over a cache of 8-bit pages, tiles of 128 rows: prompts and the pixels of frames.
+//
+// A block has 128 rows of one sequence and head, four waves 32 each.  A page's codes are made halves once, on their way to LDS (the next
+// page's are loaded while this one is worked on), and read by the four waves.  Per page and wave: 64 x 32 products of the keys with the
+// queries (v_mfma_f32_32x32x16_f16, the queries stay in registers), the weights, as many products with the values; the weights need not leave
+// the registers they come to be in (attend_device.h).
+// Rows of LDS are 16-byte chunks that are permuted by their row (chunk ^ row), so that neither the reads of 16 rows side by side nor the
+// writes meet in a bank.
+#include "attend_device.h"
+
+namespace mdcnn {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPage = MDCNN_PAGE_TOKENS;
+
+// LDS of a page: keys [64 rows][pitch of a power of two] and values [DP rows][64], as halves, and what the mask adds to a token.
+template <int DP>
+struct Stage {
+    static constexpr int kRow = DP <= 32 ? 32 : DP <= 64 ? 64 : DP <= 128 ? 128 : 256;     // halves of a row of keys
+    static constexpr int kKeys = kPage * kRow, kValues = DP * kPage;
+    static constexpr int kBytes = (kKeys + kValues) * 2 + kPage * 4;
+    // rows of the first product: MFMA row m of tile a is row 32 a + m, token 32 (m / 4 % 2) + 16 a + 4 (m / 8) + m % 4
+    __device__ static __forceinline__ int row_of(int t) { return 32 * (t >> 4 & 1) + 8 * (t >> 2 & 3) + 4 * (t >> 5) + (t & 3); }
+    __device__ static __forceinline__ int key_at(int row, int chunk) {
+        constexpr int kChunks = kRow / 8, kShift = kChunks == 4 ? 2 : kChunks == 8 ? 1 : 0;
+        return row * kRow + ((chunk ^ (row >> kShift & (kChunks < 16 ? kChunks - 1 : 15))) << 3);
+    }
+    __device__ static __forceinline__ int value_at(int d, int chunk) { return kKeys + d * kPage + ((chunk ^ (d >> 1 & 7)) << 3); }
+};
+
+// Waves to a SIMD: two where queries, sums and weights leave room for them.
+template <typename T, int DP>
+__global__ __launch_bounds__(kThreads, DP <= (sizeof(T) == 4 ? 96 : 128) ? 2 : 1) void k_attend_tiles(AttendJob j) {
+    constexpr bool kTwo = sizeof(T) == 4;
+    constexpr int NS = DP / 16, ND = DP / 32, NL = DP / 32;               // steps of channels, tiles of channels, 16-byte loads of a thread
+    using S = Stage<DP>;
+    extern __shared__ __align__(16) unsigned char lds[];
+    unsigned b = blockIdx.x;
+    const int head = b % j.heads;
+    b /= j.heads;
+    const int split = b % j.splits;
+    b /= j.splits;
+    const int seq = b % j.n_seq, tile = j.tiles - 1 - b / j.n_seq;         // the last tiles see most: they begin first
+    Rows s;
+    if (!s.load(j, seq)) return;
+    const int r0 = tile * kAttendTile, r1 = min(r0 + kAttendTile, s.rows);
+    if (r0 >= s.rows) return;
+    const Run run(j, s, r0, r1, split);
+    if (split > 0 && run.first >= run.last) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
+
+    const int row = r0 + 32 * wave + n, query = row / j.group;
+    const bool live = row < s.rows;
+    half8 qh[NS], ql[kTwo ? NS : 1];
+    int e;
+    {
+        const T* q = (const T*)j.q + (s.q0 + (live ? query : 0)) * j.q_token + (long long)(head * j.group + (live ? row % j.group : 0)) * j.q_head;
+        float top = 0.f;
+#pragma unroll
+        for (int st = 0; st < NS; ++st)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = 16 * st + 8 * half + i;
+                top = fmaxf(top, live && c < j.dim ? fabsf(to_f32(q[c])) : 0.f);
+            }
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        e = exponent_of(top);
+#pragma unroll
+        for (int st = 0; st < NS; ++st)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = 16 * st + 8 * half + i;
+                float x = live && c < j.dim ? scaled(to_f32(q[c]), -e) : 0.f;
+                x = j.scale < 0.f ? -x : x;
+                qh[st][i] = (_Float16)x;
+                if constexpr (kTwo) ql[st][i] = (_Float16)(x - (float)qh[st][i]);
+            }
+    }
+    const float logit = scaled(fabsf(j.scale) * kLog2E, e);
+    const int hi = live ? s.hi(j, query) : 0, lo = live ? s.lo(j, query) : 0;
+    // of the wave's rows: what every one sees, what any one sees
+    const int w0 = min(r0 + 32 * wave, s.rows - 1) / j.group, w1 = min(r0 + 32 * wave + 31, s.rows - 1) / j.group;
+    const bool any_row = r0 + 32 * wave < s.rows;
+    const int all_hi = s.hi(j, w0), all_lo = s.lo(j, w1), any_hi = any_row ? s.hi(j, w1) : 0, any_lo = s.lo(j, w0);
+    const uint8_t* mask = j.mask ? j.mask + seq * j.mask_row : nullptr;
+
+    float top = -INFINITY, sum = 0.f;                      // T and sum of this lane's row
+    ValueScale val;
+    float16v out[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) out[d][i] = 0.f;
+
+    const int* table = j.table + (long long)seq * j.max_pages;
+    auto page_at = [&](int p) {
+        const int id = p < run.last ? table[p] : -1;
+        return id >= 0 && id < j.pages ? id : -1;
+    };
+    // a thread's loads: 16 codes of a key or of a channel's values each, consecutive ones side by side
+    constexpr int kKeyLoads = kPage * DP / 16;
+    uint4v codes[NL];
+    unsigned char seen_byte = 1;
+    auto load = [&](int id, int p) {
+        const long long at = ((long long)max(id, 0) * j.heads + head) * (kPage * DP);
+#pragma unroll
+        for (int q = 0; q < NL; ++q) {
+            const int i = threadIdx.x + kThreads * q;
+            codes[q] = *(const uint4v*)((i < kKeyLoads ? j.k_codes : j.v_codes - kPage * DP) + at + 16 * i);
+        }
+        if (mask && threadIdx.x < kPage) seen_byte = p * kPage + (int)threadIdx.x < s.len ? mask[p * kPage + threadIdx.x] : 0;
+    };
+    auto stage = [&](_Float16* to) {
+#pragma unroll
+        for (int q = 0; q < NL; ++q) {
+            const int i = threadIdx.x + kThreads * q;
+            int a, c;
+            if (i < kKeyLoads) {
+                const int r = S::row_of(i / (DP / 16)), chunk = i % (DP / 16) * 2;
+                a = S::key_at(r, chunk);
+                c = S::key_at(r, chunk + 1);
+            } else {
+                const int k = i - kKeyLoads, d = k / (kPage / 16), chunk = k % (kPage / 16) * 2;
+                a = S::value_at(d, chunk);
+                c = S::value_at(d, chunk + 1);
+            }
+            *(half8*)(to + a) = halves_of(codes[q][0], codes[q][1]);
+            *(half8*)(to + c) = halves_of(codes[q][2], codes[q][3]);
+        }
+        if (mask && threadIdx.x < kPage) ((float*)(to + S::kKeys + S::kValues))[threadIdx.x] = seen_byte ? 0.f : -INFINITY;
+    };
+    int id = page_at(run.first), next = page_at(run.first + 1);
+    _Float16* now = (_Float16*)lds;
+    _Float16* then = (_Float16*)(lds + S::kBytes);
+    if (run.first < run.last) {
+        load(id, run.first);
+        stage(now);
+    }
+    __syncthreads();
+    for (int p = run.first; p < run.last; ++p) {
+        const int after = page_at(p + 2);
+        if (p + 1 < run.last) load(next, p + 1);
+        const int pos = p * kPage;
+        if (id >= 0 && pos < any_hi && pos + kPage > any_lo) {
+            const long long at = (long long)id * j.heads + head;
+            const float ks = j.k_scale[at], vs = j.v_scale[at];
+            float16v x[2];
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+                if (mask) {
+                    const float* add = (const float*)(now + S::kKeys + S::kValues) + 32 * half + 16 * a;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[a][i] = add[i];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[a][i] = 0.f;
+                }
+#pragma unroll
+                for (int st = 0; st < NS; ++st) {
+                    const half8 k = *(const half8*)(now + S::key_at(32 * a + n, 2 * st + half));
+                    x[a] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qh[st], x[a], 0, 0, 0);
+                    if constexpr (kTwo) x[a] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, ql[st], x[a], 0, 0, 0);
+                }
+            }
+            // x[a][i] is token 32 half + 16 a + i
+            const float by = factor_of(logit, ks);
+            val.next(vs);
+            if (pos < all_lo || pos + kPage > all_hi) {
+                const int from = lo - pos - 32 * half, to = hi - pos - 32 * half;
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (16 * a + i < from || 16 * a + i >= to) x[a][i] = -INFINITY;
+            }
+            float m = fmaxf(x[0][0], x[1][0]);
+#pragma unroll
+            for (int i = 1; i < 16; ++i) m = fmaxf(m, fmaxf(x[0][i], x[1][i]));
+            m = fmaxf(m, __shfl_xor(m, 32, 64));
+            m = m * by + val.log;
+            if (__any(m > top + kSlack)) {
+                const float next_top = fmaxf(top, m), fade = next_top == -INFINITY ? 1.f : exp2_fast(top - next_top);
+                top = next_top;
+                sum *= fade;
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) out[d][i] *= fade;
+            }
+            const float base = val.log - (top == -INFINITY ? 0.f : top);
+            const bool odd = ks != ks || val.bad || val.none;         // rare: weights one by one
+            float add = 0.f;
+            half8 ph[4], pl[kTwo ? 4 : 1];
+#pragma unroll
+            for (int t = 0; t < 32; ++t) {
+                float w = exp2_fast(__builtin_fmaf(x[t / 16][t % 16], by, base));
+                const bool hidden = x[t / 16][t % 16] == -INFINITY;
+                if (odd) w = hidden ? 0.f : w;             // a hidden token's scales do not matter
+                add += w;
+                if (odd) w = val.none ? 0.f : val.bad && !hidden ? vs : w;
+                ph[t / 8][t % 8] = (_Float16)w;
+                if constexpr (kTwo) pl[t / 8][t % 8] = (_Float16)(w - (float)ph[t / 8][t % 8]);
+            }
+            sum += add * val.inverse;
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int st = 0; st < 4; ++st) {
+                    const half8 v = *(const half8*)(now + S::value_at(32 * d + n, 4 * half + st));
+                    out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph[st], out[d], 0, 0, 0);
+                    if constexpr (kTwo) out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl[st], out[d], 0, 0, 0);
+                }
+        }
+        if (p + 1 < run.last) stage(then);
+        __syncthreads();
+        _Float16* swap = now;
+        now = then;
+        then = swap;
+        id = next;
+        next = after;
+    }
+    if (!live) return;
+    sum += __shfl_xor(sum, 32, 64);
+    const bool whole = run.splits <= 1;
+    const long long slot = ((((long long)seq * j.heads + head) * j.tiles + tile) * j.splits + split) * kAttendTile + 32 * wave + n;
+    const float inv = whole ? (top == -INFINITY && sum == 0.f ? 0.f : 1.f / sum) : 1.f;
+    T* y = (T*)j.y + (s.q0 + query) * j.y_token + (long long)(head * j.group + row % j.group) * j.y_head;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int c = 32 * d + 8 * q + 4 * half;       // four channels beside one another
+            if (!whole) {
+                *(float4v*)(j.part_out + slot * DP + c) = float4v{out[d][4 * q], out[d][4 * q + 1], out[d][4 * q + 2], out[d][4 * q + 3]};
+            } else if (c < j.dim) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[c + i] = (T)(out[d][4 * q + i] * inv);
+            }
+        }
+    if (half == 0) {
+        if (!whole) j.part_top[slot] = float2{top, sum};
+        else if (j.lse) j.lse[(s.q0 + query) * (j.heads * j.group) + head * j.group + row % j.group] = kLn2 * (top + __log2f(sum));
+    }
+}
+
+struct Tiles {
+    template <typename T, int DP>
+    static hipError_t go(const AttendJob& j, hipStream_t st) {
+        if constexpr (sizeof(T) == 4 && DP > 192) return hipErrorInvalidValue;           // (no registers for them: attend_tiles_fit)
+        else return tiles<T, DP>(j, st);
+    }
+    template <typename T, int DP>
+    static hipError_t tiles(const AttendJob& j, hipStream_t st) {
+        constexpr int kLds = 2 * Stage<DP>::kBytes;
+        const auto kern = k_attend_tiles<T, DP>;
+        if (kLds > 64 * 1024) {
+            const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+            if (err != hipSuccess) return err;
+        }
+        kern<<<(unsigned)((long long)j.splits * j.tiles * j.n_seq * j.heads), kThreads, kLds, st>>>(j);
+        return hipGetLastError();
+    }
+};
+
+}  // namespace
+
+bool attend_tiles_fit(int dtype, int pitch) { return dtype != MDCNN_F32 || pitch <= 192; }
+hipError_t launch_attend_tiles(const AttendJob& j, int dtype, hipStream_t st) { return for_type_and_pitch<Tiles>(j, dtype, st); }
+
+}  // namespace mdcnn

@@ -229,23 +229,27 @@ mdcnn_status check_attend(const mdcnn_cache_desc* c, const mdcnn_attend_desc* a,
     return MDCNN_OK;
 }
 
-// Tiles of 16 rows, and pages to a split: blocks for four to a compute unit, runs of 4 to 32 pages (a wave has a quarter of them).
-mdcnn_status plan_attend(const mdcnn_cache_desc& c, const mdcnn_attend_desc& a, int q_heads, AttendJob& j, size_t* bytes) {
+// Rows to a block and pages to a split.  Up to 32 rows go by sixteen, one or two blocks that each read the cache; more by 128, whose codes are
+// read once and made halves once.  Splits: blocks for two to four of a compute unit's places, but runs of pages long enough for what
+// a block does once (its queries, its sums).
+mdcnn_status plan_attend(const mdcnn_cache_desc& c, const mdcnn_attend_desc& a, int q_heads, int dtype, AttendJob& j, size_t* bytes) {
     j.pages = c.pages; j.heads = c.heads; j.group = q_heads / c.heads; j.dim = c.dim; j.pitch = mdcnn_cache_pitch(c.dim);
     j.n_seq = c.n_seq; j.max_pages = c.pages ? c.max_pages : 0;
     j.tokens = a.tokens; j.max_new = std::min(a.max_new, a.tokens); j.max_len = a.max_len;
     j.causal = a.causal; j.window = a.window; j.scale = a.scale;
-    const long long rows = (long long)j.max_new * j.group, columns = (rows + 15) / 16 * c.n_seq * c.heads;
-    if (rows > 0x7fffffffll || rows * c.n_seq * c.heads > 0x7fffffffll) return fail(MDCNN_ERR_SIZE, "cache_attend: too many rows");
-    j.tiles = (int)((rows + 15) / 16);
+    const long long rows = (long long)j.max_new * j.group;
+    if (rows > 0x7fffff00ll || rows * c.n_seq * c.heads > 0x7fffffffll) return fail(MDCNN_ERR_SIZE, "cache_attend: too many rows");
+    j.tile_rows = rows <= 32 || !attend_tiles_fit(dtype, j.pitch) ? kAttendRows : kAttendTile;
+    j.tiles = (int)((rows + j.tile_rows - 1) / j.tile_rows);
+    const long long columns = (long long)j.tiles * c.n_seq * c.heads;
     long long most = std::min<long long>((a.max_len + (long long)MDCNN_PAGE_TOKENS - 1) / MDCNN_PAGE_TOKENS, c.max_pages);
     if (a.window) most = std::min<long long>(most, (a.window + (long long)j.max_new + 2 * MDCNN_PAGE_TOKENS - 2) / MDCNN_PAGE_TOKENS);
     most = std::max(most, 1ll);
-    j.run = (int)std::min(32ll, std::max(4ll, columns ? most * columns / 1024 : 1ll));
+    j.run = j.tile_rows == kAttendRows ? (int)std::min(32ll, std::max(4ll, most * columns / 1024)) : (int)std::min(most, std::max(16ll, most * columns / 2048));
     j.splits = (int)((most + j.run - 1) / j.run);
-    if (columns >= 2048) { j.splits = 1; j.run = 1 << 30; }
+    if (columns >= (j.tile_rows == kAttendRows ? 2048 : 1024)) { j.splits = 1; j.run = 1 << 30; }
     if (columns * j.splits > 0x7fffffffll) return fail(MDCNN_ERR_SIZE, "cache_attend: too large");
-    *bytes = j.splits > 1 ? (size_t)columns * j.splits * 16 * (8 + 4 * (size_t)j.pitch) + 256 : 0;
+    *bytes = j.splits > 1 ? (size_t)columns * j.splits * j.tile_rows * (8 + 4 * (size_t)j.pitch) + 256 : 0;
     return MDCNN_OK;
 }
 
@@ -364,12 +368,13 @@ mdcnn_status mdcnn_cache_read(const mdcnn_cache_desc* c, const mdcnn_heads* k, c
     return run_cache(c, k, v, tokens, starts_dev, first_dev, max_new, dtype, false, stream);
 }
 
-mdcnn_status mdcnn_cache_attend_bytes(const mdcnn_cache_desc* c, const mdcnn_attend_desc* a, int q_heads, size_t* bytes) {
+mdcnn_status mdcnn_cache_attend_bytes(const mdcnn_cache_desc* c, const mdcnn_attend_desc* a, int q_heads, int dtype, size_t* bytes) {
     mdcnn_status st = check_attend(c, a, q_heads);
     if (st) return st;
+    if (!known_dtype(dtype)) return fail(MDCNN_ERR_DTYPE, "cache_attend_bytes: unknown dtype %d", dtype);
     if (!bytes) return fail(MDCNN_ERR_NULL, "cache_attend_bytes: bytes is NULL");
     AttendJob j{};
-    return plan_attend(*c, *a, q_heads, j, bytes);
+    return plan_attend(*c, *a, q_heads, dtype, j, bytes);
 }
 
 mdcnn_status mdcnn_cache_attend(const mdcnn_cache_desc* c, const mdcnn_attend_desc* a, const mdcnn_heads* q, int dtype, float* lse_dev, void* work_dev, size_t work_bytes, void* stream) {
@@ -379,7 +384,7 @@ mdcnn_status mdcnn_cache_attend(const mdcnn_cache_desc* c, const mdcnn_attend_de
     if (!known_dtype(dtype)) return fail(MDCNN_ERR_DTYPE, "cache_attend: unknown dtype %d", dtype);
     AttendJob j{};
     size_t need = 0;
-    st = plan_attend(*c, *a, q->heads, j, &need);
+    st = plan_attend(*c, *a, q->heads, dtype, j, &need);
     if (st) return st;
     if (!c->n_seq || !a->tokens || !a->max_new) return MDCNN_OK;
     st = check_heads(*q, "cache_attend", "the queries", c->dim, a->tokens, storage_bytes(dtype), true, true);
@@ -393,8 +398,11 @@ mdcnn_status mdcnn_cache_attend(const mdcnn_cache_desc* c, const mdcnn_attend_de
     j.starts = a->starts_dev; j.lengths = a->lengths_dev; j.mask = a->mask_dev; j.mask_row = a->mask_row;
     j.mask_whole = aligned(a->mask_dev, 16) && (c->n_seq == 1 || a->mask_row % 16 == 0);
     j.part_out = (float*)work_dev;
-    j.part_top = (float2*)((char*)work_dev + (size_t)j.n_seq * j.heads * j.tiles * j.splits * 16 * j.pitch * 4);
-    return launched(launch_attend_rows(j, dtype, (hipStream_t)stream), "cache_attend");
+    j.part_top = (float2*)((char*)work_dev + (size_t)j.n_seq * j.heads * j.tiles * j.splits * j.tile_rows * j.pitch * 4);
+    const auto first = j.tile_rows == kAttendRows ? launch_attend_rows : launch_attend_tiles;
+    hipError_t err = first(j, dtype, (hipStream_t)stream);
+    if (err == hipSuccess) err = launch_attend_join(j, dtype, (hipStream_t)stream);
+    return launched(err, "cache_attend");
 }
 
 }  // extern "C"

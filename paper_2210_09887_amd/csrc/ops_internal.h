@@ -91,15 +91,20 @@ struct AttendJob {
     const int* starts;
     const int* lengths;
     const uint8_t* mask;
-    float2* part_top;            // [seq][head][tile][split][16]: maximum and sum of a row
+    float2* part_top;            // [seq][head][tile][split][tile_rows]: T and sum of a row
     float* part_out;             // [..][16][pitch]
     long long q_token, q_head, y_token, y_head, mask_row;
     int pages, heads, group, dim, pitch, n_seq, max_pages;   // group: query heads to a head of the cache
     int tokens, max_new, max_len, causal, window;
     int mask_whole;              // rows of the mask begin on 16 bytes
+    int tile_rows;               // rows of a block
     int tiles, splits, run;      // tiles of rows and splits of a sequence and head (bounds), pages to a split
     float scale;
 };
 hipError_t launch_attend_rows(const AttendJob& j, int dtype, hipStream_t st);
+bool attend_tiles_fit(int dtype, int pitch);             // whether launch_attend_tiles takes them
+hipError_t launch_attend_tiles(const AttendJob& j, int dtype, hipStream_t st);
+hipError_t launch_attend_join(const AttendJob& j, int dtype, hipStream_t st);     // nothing if there is one split
+constexpr int kAttendRows = 16, kAttendTile = 128;       // rows of a block of the two
 
 }  // namespace mdcnn

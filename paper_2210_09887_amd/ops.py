@@ -304,7 +304,7 @@ class GpuCache:
             _need(mask.dtype in (torch.uint8, torch.bool) and mask.dim() == 2 and mask.shape[0] == c.n_seq and mask.shape[1] >= max_len and mask.stride(1) == 1 and mask.stride(0) >= max_len,
                   f"mask: uint8 or bool [{c.n_seq}, {max_len} or more]")
             how.mask_dev, how.mask_row = mask.data_ptr(), mask.stride(0)
-        n = B.mdcnn_cache_attend_bytes(c, how, shape[1])
+        n = B.mdcnn_cache_attend_bytes(c, how, shape[1], _DTYPE[q.dtype])
         work = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
         lse = torch.empty(shape[:2], dtype=torch.float32, device=dev)
         _call(B.mdcnn_cache_attend, dev, c, how, _heads("q", q, out, shape), _DTYPE[q.dtype], lse.data_ptr(), _ptr(work), n)

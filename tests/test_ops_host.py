@@ -148,5 +148,6 @@ def test_attend_arguments(change, status):
 
 def test_attend_workspace():
     c, a = cache(max_pages=2000), attending(max_len=100000)
-    assert B.mdcnn_cache_attend_bytes(c, a, 8) > 0 and B.mdcnn_cache_attend_bytes(c, attending(max_len=100), 8) == 0
-    refused(2, B.mdcnn_cache_attend_bytes, c, a, 6)
+    assert B.mdcnn_cache_attend_bytes(c, a, 8, 1) > 0 and B.mdcnn_cache_attend_bytes(c, attending(max_len=100), 8, 1) == 0
+    refused(2, B.mdcnn_cache_attend_bytes, c, a, 6, 1)
+    refused(3, B.mdcnn_cache_attend_bytes, c, a, 8, 7)
