@@ -94,8 +94,51 @@ __device__ __forceinline__ float factor_of(float logit, float ks) {
     const float by = logit * ks;
     return by < 1e-30f ? 1e-30f : by;
 }
-// How far a weight may lie above one before its row's T is moved (weights are halves): sums are rescaled on few pages only.
-constexpr float kSlack = 8.f;
+// T of a row is moved - and what has been summed faded - only where the weights of a lane add up to more than this (they have to be
+// halves): weights are made before anyone looks for a maximum, and on nearly all pages no one does.
+constexpr float kMuch = 16384.f;
+
+// Whether it holds in one of the lanes n and n + 32 (n, n + 16, n + 32, n + 48) that share a row.
+__device__ __forceinline__ bool row_of_two(bool here, int n) {
+    const unsigned long long b = __ballot(here);
+    return ((b | b >> 32) >> n & 1) != 0;
+}
+__device__ __forceinline__ bool row_of_four(bool here, int n) {
+    unsigned long long b = __ballot(here);
+    b |= b >> 32;
+    return ((b | b >> 16) >> n & 1) != 0;
+}
+
+// The larger one of the two lanes 32 (16) apart, in both.
+__device__ __forceinline__ float max_over_32(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_over_16(float v) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
+
+// Page numbers of a run, asked for in ascending order: 64 of them in a register of the wave.  (A scalar load for each would be waited for
+// together with whatever LDS reads are on their way.)
+struct PageIds {
+    const int* table;
+    int ids, begin, last, pages, lane;
+    __device__ __forceinline__ PageIds(const AttendJob& j, int seq, const Run& run, int first, int lane_) : table(j.table + (long long)seq * j.max_pages), last(run.last), pages(j.pages), lane(lane_) { fetch(first); }
+    __device__ __forceinline__ void fetch(int p) {
+        begin = p;
+        ids = p + lane < last ? table[p + lane] : -1;
+        ids = ids >= 0 && ids < pages ? ids : -1;
+    }
+    // -1: no page
+    __device__ __forceinline__ int at(int p) {
+        if (p >= last) return -1;
+        if (p - begin >= 64) fetch(p);
+        return __builtin_amdgcn_readlane(ids, p - begin);
+    }
+};
 
 // The power of two that brings the largest magnitude of a row to 2^13 .. 2^14 (1 for none, or one that is not finite).
 __device__ __forceinline__ int exponent_of(float top) {
@@ -103,6 +146,27 @@ __device__ __forceinline__ int exponent_of(float top) {
     return top > 0.f && e < 255 ? e - 127 - 13 : 0;
 }
 __device__ __forceinline__ float scaled(float x, int e) { return ldexpf(x, e); }
+
+// Eight channels of a query from c on (dim is a multiple of eight), zeros beyond.
+template <typename T>
+__device__ __forceinline__ void eight_of(const T* q, int c, int dim, bool whole, float (&f)[8]) {
+    if (c >= dim) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = 0.f;
+    } else if (whole) {                                    // on 16 bytes
+        constexpr int N = 16 / sizeof(T);
+#pragma unroll
+        for (int k = 0; k < 8 / N; ++k) {
+            float g[N];
+            unpack(*(const Pack<T, N>*)(q + c + N * k), g);
+#pragma unroll
+            for (int i = 0; i < N; ++i) f[N * k + i] = g[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = to_f32(q[c + i]);
+    }
+}
 
 // Which of 16 tokens from `pos` on have a nonzero byte, as bits.
 __device__ __forceinline__ unsigned mask_bits(const uint8_t* row, int pos, int end, bool whole) {

@@ -53,21 +53,19 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
     {
         float f[NS][8], top = 0.f;
 #pragma unroll
-        for (int st = 0; st < NS; ++st)
+        for (int st = 0; st < NS; ++st) {
+            eight_of(q, st < 2 * U ? 64 * (st / 2) + 16 * quad + 8 * (st & 1) : 64 * U + 8 * quad, live ? j.dim : 0, j.q_whole, f[st]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int c = (st < 2 * U ? 64 * (st / 2) + 16 * quad + 8 * (st & 1) : 64 * U + 8 * quad) + i;
-                f[st][i] = live && c < j.dim ? to_f32(q[c]) : 0.f;
-                top = fmaxf(top, fabsf(f[st][i]));
-            }
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[st][i]));
+        }
+        top = max_over_32(max_over_16(top));
         e = exponent_of(top);
+        const float sign = j.scale < 0.f ? -1.f : 1.f;
 #pragma unroll
         for (int st = 0; st < NS; ++st)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float x = scaled(j.scale < 0.f ? -f[st][i] : f[st][i], -e);
+                const float x = scaled(f[st][i], -e) * sign;
                 qh[st][i] = (_Float16)x;
                 if constexpr (kTwo) ql[st][i] = (_Float16)(x - (float)qh[st][i]);
             }
@@ -83,14 +81,19 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
 #pragma unroll
     for (int v = 0; v < NV; ++v) out[v] = float4v{0.f, 0.f, 0.f, 0.f};
 
-    const int* table = j.table + (long long)seq * j.max_pages;
+    PageIds page(j, seq, run, run.first, lane);
     const int per_head = kPage * DP;
     uint4v kr[4][U ? U : 1];
     uint2v kx[4];
     uint4v vr[NV];
-    auto page_at = [&](int p) {
-        const int id = p < run.last ? table[p] : -1;
-        return id >= 0 && id < j.pages ? id : -1;
+    // Scales come by vector loads ahead of the keys, whose return they do not wait for.
+    int beside;
+    asm("v_mov_b32 %0, 0" : "=v"(beside));
+    float ks = 0.f, vs = 0.f;
+    auto load_scales = [&](int id) {
+        const long long at = (long long)max(id, 0) * j.heads + head + beside;
+        ks = j.k_scale[at];
+        vs = j.v_scale[at];
     };
     // (no page: what the first one holds, which is then not looked at; there is one wherever there is a run)
     auto load_keys = [&](int id) {
@@ -108,22 +111,22 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
 #pragma unroll
         for (int t = 0; t < NV; ++t) vr[t] = *(const uint4v*)(v + (16 * t + n) * kPage + 16 * quad);
     };
-    int p = run.first + wave, id = page_at(p), next = page_at(p + kWaves);
+    int p = run.first + wave, id = page.at(p), next = page.at(p + kWaves);
     if (p < run.last) {
+        load_scales(id);
         load_keys(id);
         load_values(id);
     }
     for (; p < run.last; p += kWaves) {
-        const int after = page_at(p + 2 * kWaves);
+        const int after = page.at(p + 2 * kWaves);
         if (id < 0) {                                      // no page: its tokens do not exist
             id = next;
             next = after;
+            load_scales(id);
             load_keys(id);
             load_values(id);
             continue;
         }
-        const long long at = (long long)id * j.heads + head;
-        const float ks = j.k_scale[at], vs = j.v_scale[at];
         float4v acc[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -136,9 +139,10 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
             }
             __builtin_amdgcn_sched_barrier(0);             // or all codes are made halves first, in as many registers
         }
+        const float by = factor_of(logit, uniform(ks)), vs_now = uniform(vs);
+        load_scales(next);
         load_keys(next);
-        const float by = factor_of(logit, ks);
-        val.next(vs);
+        val.next(vs_now);
         float x[16];
 #pragma unroll
         for (int t = 0; t < 16; ++t) x[t] = acc[t / 4][t % 4];
@@ -152,42 +156,59 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
                 x[t] = seen >> t & 1 ? x[t] : -INFINITY;
             }
         }
-        float m = x[0];
+        if (by == by) {
+            // weights, at first as if T stayed
+            float add;
+            half8 ph[2], pl[kTwo ? 2 : 1];
+            auto weigh = [&]() {
+                const float base = val.log - (top == -INFINITY ? 0.f : top);
+                float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int t = 1; t < 16; ++t) m = fmaxf(m, x[t]);
-        m = fmaxf(m, __shfl_xor(m, 16, 64));
-        m = fmaxf(m, __shfl_xor(m, 32, 64));
-        m = m * by + val.log;
-        if (__any(m > top + kSlack)) {
-            const float next_top = fmaxf(top, m), fade = next_top == -INFINITY ? 1.f : exp2_fast(top - next_top);
-            top = next_top;
-            sum *= fade;
+                for (int t = 0; t < 16; ++t) {
+                    const float w = exp2_fast(__builtin_fmaf(x[t], by, base));
+                    part[t % 4] += w;
+                    ph[t / 8][t % 8] = (_Float16)w;
+                    if constexpr (kTwo) pl[t / 8][t % 8] = (_Float16)(w - (float)ph[t / 8][t % 8]);
+                }
+                add = (part[0] + part[1]) + (part[2] + part[3]);
+            };
+            weigh();
+            bool moves = add > kMuch || (live && top == -INFINITY);
+            if (__any(moves)) {
+                moves = row_of_four(moves, n);
+                float m[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-            for (int v = 0; v < NV; ++v) out[v] *= fade;
-        }
-        const float base = val.log - (top == -INFINITY ? 0.f : top);
-        float add = 0.f;
-        half8 ph[2], pl[kTwo ? 2 : 1];
+                for (int t = 4; t < 16; ++t) m[t % 4] = fmaxf(m[t % 4], x[t]);
+                const float most = max_over_32(max_over_16(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])))) * by + val.log, next_top = moves ? fmaxf(top, most) : top;
+                const float fade = top == -INFINITY ? 1.f : exp2_fast(top - next_top);           // (nothing summed so far: nothing to fade)
+                top = next_top;
+                sum *= fade;
 #pragma unroll
-        for (int t = 0; t < 16; ++t) {
-            float w = exp2_fast(__builtin_fmaf(x[t], by, base));
-            w = seen >> t & 1 ? w : 0.f;                   // (whatever the scales of a hidden token are)
-            add += w;
-            w = val.none ? 0.f : val.bad && seen >> t & 1 ? vs : w;
-            ph[t / 8][t % 8] = (_Float16)w;
-            if constexpr (kTwo) pl[t / 8][t % 8] = (_Float16)(w - (float)ph[t / 8][t % 8]);
-        }
-        sum += add * val.inverse;
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const half8 a = halves_of(vr[v][0], vr[v][1]), b = halves_of(vr[v][2], vr[v][3]);
-            out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, ph[0], out[v], 0, 0, 0);
-            out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, ph[1], out[v], 0, 0, 0);
-            if constexpr (kTwo) {
-                out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, pl[0], out[v], 0, 0, 0);
-                out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, pl[1], out[v], 0, 0, 0);
+                for (int v = 0; v < NV; ++v) out[v] *= fade;
+                weigh();
             }
-            if (v % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            sum += add * val.inverse;
+            if (val.bad) {
+                const bool bad = row_of_four(seen != 0, n);
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) out[v][i] = bad ? vs_now : out[v][i];
+            } else if (!val.none) {
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    const half8 a = halves_of(vr[v][0], vr[v][1]), b = halves_of(vr[v][2], vr[v][3]);
+                    out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, ph[0], out[v], 0, 0, 0);
+                    out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, ph[1], out[v], 0, 0, 0);
+                    if constexpr (kTwo) {
+                        out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, pl[0], out[v], 0, 0, 0);
+                        out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, pl[1], out[v], 0, 0, 0);
+                    }
+                    if (v % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        } else {                                           // the row sees tokens whose scale is not a number
+            sum = row_of_four(seen != 0, n) ? by : sum;
         }
         id = next;
         next = after;
@@ -228,55 +249,63 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
     }
 }
 
-// Joins the splits of a row; a block to a row: threads over its channels, four of them each, and over the splits.
+// Joins the splits of rows.  A thread has four channels of a row and every j.sets-th split; a block as many rows as it has threads for.
 template <typename T, int DP>
 __global__ __launch_bounds__(kThreads) void k_attend_join(AttendJob j) {
-    constexpr int kLanes = DP / 4, kSets = kThreads / kLanes;
-    __shared__ float4v s_part[kSets][kLanes];
-    __shared__ float s_sum[kSets];
-    const int per = j.max_new * j.group;
-    const int r = blockIdx.x % per, head = blockIdx.x / per % j.heads, seq = blockIdx.x / per / j.heads;
+    constexpr int kLanes = DP / 4;
+    __shared__ float4v s_part[kThreads];
+    __shared__ float2 s_top[kThreads];
+    const int per_block = kThreads / (kLanes * j.sets), blocks = (j.max_new * j.group + per_block - 1) / per_block;
+    const int c = threadIdx.x % kLanes, set = threadIdx.x / kLanes % j.sets, slot_row = threadIdx.x / (kLanes * j.sets);
+    const int r = blockIdx.x % blocks * per_block + slot_row, head = blockIdx.x / blocks % j.heads, seq = blockIdx.x / blocks / j.heads;
     Rows s;
-    if (!s.load(j, seq) || r >= s.rows) return;
+    const bool any = s.load(j, seq);
     const int tile = r / j.tile_rows, m = r % j.tile_rows;
-    const Run run(j, s, tile * j.tile_rows, min((tile + 1) * j.tile_rows, s.rows), 0);
-    if (run.splits <= 1) return;
+    bool on = any && slot_row < per_block && r < s.rows;
+    int splits = 0;
+    if (on) splits = Run(j, s, tile * j.tile_rows, min((tile + 1) * j.tile_rows, s.rows), 0).splits;
+    on = on && splits > 1;                                 // (a single one has written the row itself)
     const long long slot = (((long long)seq * j.heads + head) * j.tiles + tile) * j.splits;
-    float peak = -INFINITY;
-    for (int z = threadIdx.x & 63; z < run.splits; z += 64) peak = fmaxf(peak, j.part_top[(slot + z) * j.tile_rows + m].x);
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) peak = fmaxf(peak, __shfl_xor(peak, k, 64));
-    const float base = peak == -INFINITY ? 0.f : peak;
-    const int set = threadIdx.x / kLanes, c = threadIdx.x % kLanes;
-    if (set < kSets) {
-        float4v x = float4v{0.f, 0.f, 0.f, 0.f};
-        float total = 0.f;
+    float top = -INFINITY, total = 0.f;
+    float4v x = float4v{0.f, 0.f, 0.f, 0.f};
+    auto take = [&](float2 t, float4v y) {
+        const float next = fmaxf(top, t.x), base = next == -INFINITY ? 0.f : next, fade = exp2_fast(top - base), w = exp2_fast(t.x - base);
+        top = next;
+        total = total * fade + t.y * w;
+        x = x * fade + y * w;
+    };
+    if (on) {
 #pragma unroll 4
-        for (int z = set; z < run.splits; z += kSets) {
-            const float2 t = j.part_top[(slot + z) * j.tile_rows + m];
-            const float w = exp2_fast(t.x - base);
-            total += w * t.y;
-            x += w * *(const float4v*)(j.part_out + ((slot + z) * j.tile_rows + m) * DP + 4 * c);
+        for (int z = set; z < splits; z += j.sets) {
+            const long long at = (slot + z) * j.tile_rows + m;
+            take(j.part_top[at], *(const float4v*)(j.part_out + at * DP + 4 * c));
         }
-        s_part[set][c] = x;
-        if (c == 0) s_sum[set] = total;
     }
-    __syncthreads();
-    if (set) return;
-    float4v x = s_part[0][c];
-    float total = s_sum[0];
-    for (int k = 1; k < kSets; ++k) { x += s_part[k][c]; total += s_sum[k]; }
-    const float inv = peak == -INFINITY && total == 0.f ? 0.f : 1.f / total;
+    if (j.sets > 1) {
+        s_part[threadIdx.x] = x;
+        s_top[threadIdx.x] = float2{top, total};
+        __syncthreads();
+        on = on && set == 0;
+        if (on)
+            for (int k = 1; k < j.sets; ++k) take(s_top[threadIdx.x + k * kLanes], s_part[threadIdx.x + k * kLanes]);
+    }
+    if (!on) return;
+    const float inv = top == -INFINITY && total == 0.f ? 0.f : 1.f / total;
     T* y = (T*)j.y + (s.q0 + r / j.group) * j.y_token + (long long)(head * j.group + r % j.group) * j.y_head;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (4 * c + i < j.dim) y[4 * c + i] = (T)(x[i] * inv);
-    if (c == 0 && j.lse) j.lse[(s.q0 + r / j.group) * (j.heads * j.group) + head * j.group + r % j.group] = kLn2 * (peak + __log2f(total));
+    if (c == 0 && j.lse) j.lse[(s.q0 + r / j.group) * (j.heads * j.group) + head * j.group + r % j.group] = kLn2 * (top + __log2f(total));
 }
 
 template <typename T, int DP>
-hipError_t launch_join(const AttendJob& j, hipStream_t st) {
-    if (j.splits > 1) k_attend_join<T, DP><<<(unsigned)((long long)j.max_new * j.group * j.n_seq * j.heads), kThreads, 0, st>>>(j);
+hipError_t launch_join(AttendJob j, hipStream_t st) {
+    if (j.splits < 2) return hipSuccess;
+    // up to eight splits to a thread, as far as a block has threads
+    j.sets = 1;
+    while (j.sets * 8 < j.splits && 2 * j.sets * (DP / 4) <= kThreads) j.sets *= 2;
+    const long long per_block = kThreads / (DP / 4 * j.sets), rows = (long long)j.max_new * j.group;
+    k_attend_join<T, DP><<<(unsigned)((rows + per_block - 1) / per_block * j.n_seq * j.heads), kThreads, 0, st>>>(j);
     return hipGetLastError();
 }
 template <typename T, int DP>

@@ -20,7 +20,7 @@ template <int DP>
 struct Stage {
     static constexpr int kRow = DP <= 32 ? 32 : DP <= 64 ? 64 : DP <= 128 ? 128 : 256;     // halves of a row of keys
     static constexpr int kKeys = kPage * kRow, kValues = DP * kPage;
-    static constexpr int kBytes = (kKeys + kValues) * 2 + kPage * 4;
+    static constexpr int kBytes = (kKeys + kValues) * 2 + kPage * 4 + 16;               // .. and the two scales
     // rows of the first product: MFMA row m of tile a is row 32 a + m, token 32 (m / 4 % 2) + 16 a + 4 (m / 8) + m % 4
     __device__ static __forceinline__ int row_of(int t) { return 32 * (t >> 4 & 1) + 8 * (t >> 2 & 3) + 4 * (t >> 5) + (t & 3); }
     __device__ static __forceinline__ int key_at(int row, int chunk) {
@@ -31,7 +31,7 @@ struct Stage {
 };
 
 // Waves to a SIMD: two where queries, sums and weights leave room for them.
-template <typename T, int DP>
+template <typename T, int DP, bool MASK>
 __global__ __launch_bounds__(kThreads, DP <= (sizeof(T) == 4 ? 96 : 128) ? 2 : 1) void k_attend_tiles(AttendJob j) {
     constexpr bool kTwo = sizeof(T) == 4;
     constexpr int NS = DP / 16, ND = DP / 32, NL = DP / 32;               // steps of channels, tiles of channels, 16-byte loads of a thread
@@ -59,24 +59,26 @@ __global__ __launch_bounds__(kThreads, DP <= (sizeof(T) == 4 ? 96 : 128) ? 2 : 1
         const T* q = (const T*)j.q + (s.q0 + (live ? query : 0)) * j.q_token + (long long)(head * j.group + (live ? row % j.group : 0)) * j.q_head;
         float top = 0.f;
 #pragma unroll
-        for (int st = 0; st < NS; ++st)
+        for (int st = 0; st < NS; ++st) {
+            float f[8];
+            eight_of(q, 16 * st + 8 * half, live ? j.dim : 0, j.q_whole, f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int c = 16 * st + 8 * half + i;
-                top = fmaxf(top, live && c < j.dim ? fabsf(to_f32(q[c])) : 0.f);
-            }
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[i]));
+        }
+        top = max_over_32(top);
         e = exponent_of(top);
+        const float sign = j.scale < 0.f ? -1.f : 1.f;
 #pragma unroll
-        for (int st = 0; st < NS; ++st)
+        for (int st = 0; st < NS; ++st) {
+            float f[8];
+            eight_of(q, 16 * st + 8 * half, live ? j.dim : 0, j.q_whole, f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int c = 16 * st + 8 * half + i;
-                float x = live && c < j.dim ? scaled(to_f32(q[c]), -e) : 0.f;
-                x = j.scale < 0.f ? -x : x;
+                const float x = scaled(f[i], -e) * sign;
                 qh[st][i] = (_Float16)x;
                 if constexpr (kTwo) ql[st][i] = (_Float16)(x - (float)qh[st][i]);
             }
+        }
     }
     const float logit = scaled(fabsf(j.scale) * kLog2E, e);
     const int hi = live ? s.hi(j, query) : 0, lo = live ? s.lo(j, query) : 0;
@@ -84,7 +86,7 @@ __global__ __launch_bounds__(kThreads, DP <= (sizeof(T) == 4 ? 96 : 128) ? 2 : 1
     const int w0 = min(r0 + 32 * wave, s.rows - 1) / j.group, w1 = min(r0 + 32 * wave + 31, s.rows - 1) / j.group;
     const bool any_row = r0 + 32 * wave < s.rows;
     const int all_hi = s.hi(j, w0), all_lo = s.lo(j, w1), any_hi = any_row ? s.hi(j, w1) : 0, any_lo = s.lo(j, w0);
-    const uint8_t* mask = j.mask ? j.mask + seq * j.mask_row : nullptr;
+    const uint8_t* mask = MASK ? j.mask + seq * j.mask_row : nullptr;
 
     float top = -INFINITY, sum = 0.f;                      // T and sum of this lane's row
     ValueScale val;
@@ -94,15 +96,12 @@ __global__ __launch_bounds__(kThreads, DP <= (sizeof(T) == 4 ? 96 : 128) ? 2 : 1
 #pragma unroll
         for (int i = 0; i < 16; ++i) out[d][i] = 0.f;
 
-    const int* table = j.table + (long long)seq * j.max_pages;
-    auto page_at = [&](int p) {
-        const int id = p < run.last ? table[p] : -1;
-        return id >= 0 && id < j.pages ? id : -1;
-    };
+    PageIds page(j, seq, run, run.first, lane);
     // a thread's loads: 16 codes of a key or of a channel's values each, consecutive ones side by side
     constexpr int kKeyLoads = kPage * DP / 16;
     uint4v codes[NL];
     unsigned char seen_byte = 1;
+    float scale = 0.f;
     auto load = [&](int id, int p) {
         const long long at = ((long long)max(id, 0) * j.heads + head) * (kPage * DP);
 #pragma unroll
@@ -110,12 +109,15 @@ __global__ __launch_bounds__(kThreads, DP <= (sizeof(T) == 4 ? 96 : 128) ? 2 : 1
             const int i = threadIdx.x + kThreads * q;
             codes[q] = *(const uint4v*)((i < kKeyLoads ? j.k_codes : j.v_codes - kPage * DP) + at + 16 * i);
         }
-        if (mask && threadIdx.x < kPage) seen_byte = p * kPage + (int)threadIdx.x < s.len ? mask[p * kPage + threadIdx.x] : 0;
+        if (threadIdx.x < 2) scale = (threadIdx.x ? j.v_scale : j.k_scale)[(long long)max(id, 0) * j.heads + head];
+        if (MASK && threadIdx.x < kPage) seen_byte = p * kPage + (int)threadIdx.x < s.len ? mask[p * kPage + threadIdx.x] : 0;
     };
     auto stage = [&](_Float16* to) {
+        int thread = threadIdx.x;
+        if (DP > 128) asm volatile("" : "+v"(thread));     // places are worked out anew for each page: registers are short
 #pragma unroll
         for (int q = 0; q < NL; ++q) {
-            const int i = threadIdx.x + kThreads * q;
+            const int i = thread + kThreads * q;
             int a, c;
             if (i < kKeyLoads) {
                 const int r = S::row_of(i / (DP / 16)), chunk = i % (DP / 16) * 2;
@@ -129,9 +131,11 @@ __global__ __launch_bounds__(kThreads, DP <= (sizeof(T) == 4 ? 96 : 128) ? 2 : 1
             *(half8*)(to + a) = halves_of(codes[q][0], codes[q][1]);
             *(half8*)(to + c) = halves_of(codes[q][2], codes[q][3]);
         }
-        if (mask && threadIdx.x < kPage) ((float*)(to + S::kKeys + S::kValues))[threadIdx.x] = seen_byte ? 0.f : -INFINITY;
+        float* beside = (float*)(to + S::kKeys + S::kValues);
+        if (threadIdx.x < 2) beside[kPage + threadIdx.x] = scale;
+        if (MASK && threadIdx.x < kPage) beside[threadIdx.x] = seen_byte ? 0.f : -INFINITY;
     };
-    int id = page_at(run.first), next = page_at(run.first + 1);
+    int id = page.at(run.first), next = page.at(run.first + 1);
     _Float16* now = (_Float16*)lds;
     _Float16* then = (_Float16*)(lds + S::kBytes);
     if (run.first < run.last) {
@@ -140,17 +144,19 @@ __global__ __launch_bounds__(kThreads, DP <= (sizeof(T) == 4 ? 96 : 128) ? 2 : 1
     }
     __syncthreads();
     for (int p = run.first; p < run.last; ++p) {
-        const int after = page_at(p + 2);
+        const int after = page.at(p + 2);
         if (p + 1 < run.last) load(next, p + 1);
         const int pos = p * kPage;
         if (id >= 0 && pos < any_hi && pos + kPage > any_lo) {
-            const long long at = (long long)id * j.heads + head;
-            const float ks = j.k_scale[at], vs = j.v_scale[at];
+            const float* beside = (const float*)(now + S::kKeys + S::kValues);
+            const float ks = uniform(beside[kPage]), vs = uniform(beside[kPage + 1]);
+            int place = n;
+            if (DP > 128) asm volatile("" : "+v"(place));
             float16v x[2];
 #pragma unroll
             for (int a = 0; a < 2; ++a) {
-                if (mask) {
-                    const float* add = (const float*)(now + S::kKeys + S::kValues) + 32 * half + 16 * a;
+                if constexpr (MASK) {
+                    const float* add = beside + 32 * half + 16 * a;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[a][i] = add[i];
                 } else {
@@ -159,14 +165,12 @@ __global__ __launch_bounds__(kThreads, DP <= (sizeof(T) == 4 ? 96 : 128) ? 2 : 1
                 }
 #pragma unroll
                 for (int st = 0; st < NS; ++st) {
-                    const half8 k = *(const half8*)(now + S::key_at(32 * a + n, 2 * st + half));
+                    const half8 k = *(const half8*)(now + S::key_at(32 * a + place, 2 * st + half));
                     x[a] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qh[st], x[a], 0, 0, 0);
                     if constexpr (kTwo) x[a] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, ql[st], x[a], 0, 0, 0);
                 }
             }
             // x[a][i] is token 32 half + 16 a + i
-            const float by = factor_of(logit, ks);
-            val.next(vs);
             if (pos < all_lo || pos + kPage > all_hi) {
                 const int from = lo - pos - 32 * half, to = hi - pos - 32 * half;
 #pragma unroll
@@ -175,43 +179,66 @@ __global__ __launch_bounds__(kThreads, DP <= (sizeof(T) == 4 ? 96 : 128) ? 2 : 1
                     for (int i = 0; i < 16; ++i)
                         if (16 * a + i < from || 16 * a + i >= to) x[a][i] = -INFINITY;
             }
-            float m = fmaxf(x[0][0], x[1][0]);
+            const float by = factor_of(logit, ks);
+            val.next(vs);
+            bool bad = false;                              // the row sees tokens whose scale is not a number
+            if (ks != ks || val.bad) {
 #pragma unroll
-            for (int i = 1; i < 16; ++i) m = fmaxf(m, fmaxf(x[0][i], x[1][i]));
-            m = fmaxf(m, __shfl_xor(m, 32, 64));
-            m = m * by + val.log;
-            if (__any(m > top + kSlack)) {
-                const float next_top = fmaxf(top, m), fade = next_top == -INFINITY ? 1.f : exp2_fast(top - next_top);
-                top = next_top;
-                sum *= fade;
-#pragma unroll
-                for (int d = 0; d < ND; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) out[d][i] *= fade;
+                for (int t = 0; t < 32; ++t) bad = bad || x[t / 16][t % 16] != -INFINITY;
+                bad = row_of_two(bad, n);
             }
-            const float base = val.log - (top == -INFINITY ? 0.f : top);
-            const bool odd = ks != ks || val.bad || val.none;         // rare: weights one by one
-            float add = 0.f;
-            half8 ph[4], pl[kTwo ? 4 : 1];
+            if (ks == ks) {
+                // weights, at first as if T stayed
+                float add;
+                half8 ph[4], pl[kTwo ? 4 : 1];
+                auto weigh = [&]() {
+                    const float base = val.log - (top == -INFINITY ? 0.f : top);
+                    float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int t = 0; t < 32; ++t) {
-                float w = exp2_fast(__builtin_fmaf(x[t / 16][t % 16], by, base));
-                const bool hidden = x[t / 16][t % 16] == -INFINITY;
-                if (odd) w = hidden ? 0.f : w;             // a hidden token's scales do not matter
-                add += w;
-                if (odd) w = val.none ? 0.f : val.bad && !hidden ? vs : w;
-                ph[t / 8][t % 8] = (_Float16)w;
-                if constexpr (kTwo) pl[t / 8][t % 8] = (_Float16)(w - (float)ph[t / 8][t % 8]);
-            }
-            sum += add * val.inverse;
+                    for (int t = 0; t < 32; ++t) {
+                        const float w = exp2_fast(__builtin_fmaf(x[t / 16][t % 16], by, base));
+                        part[t % 4] += w;
+                        ph[t / 8][t % 8] = (_Float16)w;
+                        if constexpr (kTwo) pl[t / 8][t % 8] = (_Float16)(w - (float)ph[t / 8][t % 8]);
+                    }
+                    add = (part[0] + part[1]) + (part[2] + part[3]);
+                };
+                weigh();
+                bool moves = add > kMuch || (live && top == -INFINITY);
+                if (__any(moves)) {
+                    moves = row_of_two(moves, n);
+                    float m[4] = {x[0][0], x[0][1], x[0][2], x[0][3]};
 #pragma unroll
-            for (int d = 0; d < ND; ++d)
+                    for (int t = 4; t < 32; ++t) m[t % 4] = fmaxf(m[t % 4], x[t / 16][t % 16]);
+                    const float most = max_over_32(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]))) * by + val.log, next_top = moves ? fmaxf(top, most) : top;
+                    const float fade = top == -INFINITY ? 1.f : exp2_fast(top - next_top);       // (nothing summed so far: nothing to fade)
+                    top = next_top;
+                    sum *= fade;
 #pragma unroll
-                for (int st = 0; st < 4; ++st) {
-                    const half8 v = *(const half8*)(now + S::value_at(32 * d + n, 4 * half + st));
-                    out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph[st], out[d], 0, 0, 0);
-                    if constexpr (kTwo) out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl[st], out[d], 0, 0, 0);
+                    for (int d = 0; d < ND; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) out[d][i] *= fade;
+                    weigh();
                 }
+                sum += add * val.inverse;
+                if (val.bad) {
+#pragma unroll
+                    for (int d = 0; d < ND; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) out[d][i] = bad ? vs : out[d][i];
+                } else if (!val.none) {
+#pragma unroll
+                    for (int d = 0; d < ND; ++d)
+#pragma unroll
+                        for (int st = 0; st < 4; ++st) {
+                            const half8 v = *(const half8*)(now + S::value_at(32 * d + place, 4 * half + st));
+                            out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph[st], out[d], 0, 0, 0);
+                            if constexpr (kTwo) out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl[st], out[d], 0, 0, 0);
+                        }
+                }
+            } else {
+                sum = bad ? ks : sum;
+            }
         }
         if (p + 1 < run.last) stage(then);
         __syncthreads();
@@ -249,12 +276,12 @@ struct Tiles {
     template <typename T, int DP>
     static hipError_t go(const AttendJob& j, hipStream_t st) {
         if constexpr (sizeof(T) == 4 && DP > 192) return hipErrorInvalidValue;           // (no registers for them: attend_tiles_fit)
-        else return tiles<T, DP>(j, st);
+        else return j.mask ? tiles<T, DP, true>(j, st) : tiles<T, DP, false>(j, st);
     }
-    template <typename T, int DP>
+    template <typename T, int DP, bool MASK>
     static hipError_t tiles(const AttendJob& j, hipStream_t st) {
         constexpr int kLds = 2 * Stage<DP>::kBytes;
-        const auto kern = k_attend_tiles<T, DP>;
+        const auto kern = k_attend_tiles<T, DP, MASK>;
         if (kLds > 64 * 1024) {
             const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
             if (err != hipSuccess) return err;

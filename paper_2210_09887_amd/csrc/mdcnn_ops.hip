@@ -397,6 +397,8 @@ mdcnn_status mdcnn_cache_attend(const mdcnn_cache_desc* c, const mdcnn_attend_de
     j.k_codes = c->k_dev; j.v_codes = c->v_dev; j.k_scale = c->k_scale_dev; j.v_scale = c->v_scale_dev; j.table = c->table_dev;
     j.starts = a->starts_dev; j.lengths = a->lengths_dev; j.mask = a->mask_dev; j.mask_row = a->mask_row;
     j.mask_whole = aligned(a->mask_dev, 16) && (c->n_seq == 1 || a->mask_row % 16 == 0);
+    const long long per = 16 / (long long)storage_bytes(dtype);
+    j.q_whole = aligned(q->x_dev, 16) && q->x_token % per == 0 && (q->heads == 1 || q->x_head % per == 0);
     j.part_out = (float*)work_dev;
     j.part_top = (float2*)((char*)work_dev + (size_t)j.n_seq * j.heads * j.tiles * j.splits * j.tile_rows * j.pitch * 4);
     const auto first = j.tile_rows == kAttendRows ? launch_attend_rows : launch_attend_tiles;

@@ -96,9 +96,10 @@ struct AttendJob {
     long long q_token, q_head, y_token, y_head, mask_row;
     int pages, heads, group, dim, pitch, n_seq, max_pages;   // group: query heads to a head of the cache
     int tokens, max_new, max_len, causal, window;
-    int mask_whole;              // rows of the mask begin on 16 bytes
+    int mask_whole, q_whole;     // rows of the mask, heads of the queries begin on 16 bytes
     int tile_rows;               // rows of a block
     int tiles, splits, run;      // tiles of rows and splits of a sequence and head (bounds), pages to a split
+    int sets;                    // of a row's splits when they are joined
     float scale;
 };
 hipError_t launch_attend_rows(const AttendJob& j, int dtype, hipStream_t st);
