@@ -31,18 +31,24 @@ struct Stage {
 };
 
 // Waves to a SIMD: two where queries, sums and weights leave room for them.
+// LDS is waited for, loads from memory are not.
+__device__ __forceinline__ void page_over() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Waves to a SIMD, as queries, sums, products and weights leave room for them.  More of them help: one wave issues a vector instruction every five
+// cycles, two or three together one every three.  (64 channels of 16 bits: two waves 1744 us for 4 x 4096 queries of 32 heads over 8192 tokens, three 1602.)
 template <typename T, int DP, bool MASK>
-__global__ __launch_bounds__(kThreads, DP <= (sizeof(T) == 4 ? 96 : 128) ? 2 : 1) void k_attend_tiles(AttendJob j) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (DP <= 64 ? 3 : DP <= 128 ? 2 : 1) : (DP == 32 ? 3 : DP <= 96 ? 2 : 1)) void k_attend_tiles(AttendJob j) {
     constexpr bool kTwo = sizeof(T) == 4;
     constexpr int NS = DP / 16, ND = DP / 32, NL = DP / 32;               // steps of channels, tiles of channels, 16-byte loads of a thread
+    constexpr bool kAnew = DP > 128 || (DP == 64 && MASK);                // places in LDS are worked out anew for each page: registers are short
     using S = Stage<DP>;
     extern __shared__ __align__(16) unsigned char lds[];
     unsigned b = blockIdx.x;
-    const int head = b % j.heads;
+    const int head = b % j.heads;                          // (tiles of a head on one XCD where there are eight heads)
     b /= j.heads;
-    const int split = b % j.splits;
-    b /= j.splits;
-    const int seq = b % j.n_seq, tile = j.tiles - 1 - b / j.n_seq;         // the last tiles see most: they begin first
+    const int seq = b % j.n_seq;
+    b /= j.n_seq;
+    const int tile = j.tiles - 1 - b % j.tiles, split = b / j.tiles;       // the last tiles see most: they begin first
     Rows s;
     if (!s.load(j, seq)) return;
     const int r0 = tile * kAttendTile, r1 = min(r0 + kAttendTile, s.rows);
@@ -114,7 +120,7 @@ __global__ __launch_bounds__(kThreads, DP <= (sizeof(T) == 4 ? 96 : 128) ? 2 : 1
     };
     auto stage = [&](_Float16* to) {
         int thread = threadIdx.x;
-        if (DP > 128) asm volatile("" : "+v"(thread));     // places are worked out anew for each page: registers are short
+        if (kAnew) asm volatile("" : "+v"(thread));
 #pragma unroll
         for (int q = 0; q < NL; ++q) {
             const int i = thread + kThreads * q;
@@ -151,7 +157,7 @@ __global__ __launch_bounds__(kThreads, DP <= (sizeof(T) == 4 ? 96 : 128) ? 2 : 1
             const float* beside = (const float*)(now + S::kKeys + S::kValues);
             const float ks = uniform(beside[kPage]), vs = uniform(beside[kPage + 1]);
             int place = n;
-            if (DP > 128) asm volatile("" : "+v"(place));
+            if (kAnew) asm volatile("" : "+v"(place));
             float16v x[2];
 #pragma unroll
             for (int a = 0; a < 2; ++a) {
@@ -163,12 +169,13 @@ __global__ __launch_bounds__(kThreads, DP <= (sizeof(T) == 4 ? 96 : 128) ? 2 : 1
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[a][i] = 0.f;
                 }
+            }
 #pragma unroll
-                for (int st = 0; st < NS; ++st) {
-                    const half8 k = *(const half8*)(now + S::key_at(32 * a + place, 2 * st + half));
-                    x[a] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qh[st], x[a], 0, 0, 0);
-                    if constexpr (kTwo) x[a] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, ql[st], x[a], 0, 0, 0);
-                }
+            for (int i = 0; i < 2 * NS; ++i) {             // the two sums in turn, so that neither waits for itself; where registers are short one by one
+                const int st = DP <= 128 ? i / 2 : i % NS, a = DP <= 128 ? i % 2 : i / NS;
+                const half8 k = *(const half8*)(now + S::key_at(32 * a + place, 2 * st + half));
+                x[a] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qh[st], x[a], 0, 0, 0);
+                if constexpr (kTwo) x[a] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, ql[st], x[a], 0, 0, 0);
             }
             // x[a][i] is token 32 half + 16 a + i
             if (pos < all_lo || pos + kPage > all_hi) {
@@ -193,13 +200,14 @@ __global__ __launch_bounds__(kThreads, DP <= (sizeof(T) == 4 ? 96 : 128) ? 2 : 1
                 half8 ph[4], pl[kTwo ? 4 : 1];
                 auto weigh = [&]() {
                     const float base = val.log - (top == -INFINITY ? 0.f : top);
-                    float part[4] = {0.f, 0.f, 0.f, 0.f};
+                    float part[4];
 #pragma unroll
                     for (int t = 0; t < 32; ++t) {
                         const float w = exp2_fast(__builtin_fmaf(x[t / 16][t % 16], by, base));
-                        part[t % 4] += w;
+                        part[t % 4] = t < 4 ? w : part[t % 4] + w;
                         ph[t / 8][t % 8] = (_Float16)w;
                         if constexpr (kTwo) pl[t / 8][t % 8] = (_Float16)(w - (float)ph[t / 8][t % 8]);
+                        if (t % 8 == 7) __builtin_amdgcn_sched_barrier(0);           // eight at a time: registers are short
                     }
                     add = (part[0] + part[1]) + (part[2] + part[3]);
                 };
@@ -228,20 +236,19 @@ __global__ __launch_bounds__(kThreads, DP <= (sizeof(T) == 4 ? 96 : 128) ? 2 : 1
                         for (int i = 0; i < 16; ++i) out[d][i] = bad ? vs : out[d][i];
                 } else if (!val.none) {
 #pragma unroll
-                    for (int d = 0; d < ND; ++d)
-#pragma unroll
-                        for (int st = 0; st < 4; ++st) {
-                            const half8 v = *(const half8*)(now + S::value_at(32 * d + place, 4 * half + st));
-                            out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph[st], out[d], 0, 0, 0);
-                            if constexpr (kTwo) out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl[st], out[d], 0, 0, 0);
-                        }
+                    for (int i = 0; i < 4 * ND; ++i) {
+                        const int st = DP <= 128 ? i / ND : i % 4, d = DP <= 128 ? i % ND : i / 4;
+                        const half8 v = *(const half8*)(now + S::value_at(32 * d + place, 4 * half + st));
+                        out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph[st], out[d], 0, 0, 0);
+                        if constexpr (kTwo) out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl[st], out[d], 0, 0, 0);
+                    }
                 }
             } else {
                 sum = bad ? ks : sum;
             }
         }
         if (p + 1 < run.last) stage(then);
-        __syncthreads();
+        page_over();
         _Float16* swap = now;
         now = then;
         then = swap;

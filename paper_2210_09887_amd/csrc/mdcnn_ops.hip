@@ -230,8 +230,10 @@ mdcnn_status check_attend(const mdcnn_cache_desc* c, const mdcnn_attend_desc* a,
 }
 
 // Rows to a block and pages to a split.  Up to 32 rows go by sixteen, one or two blocks that each read the cache; more by 128, whose codes are
-// read once and made halves once.  Splits: blocks for two to four of a compute unit's places, but runs of pages long enough for what
-// a block does once (its queries, its sums).
+// read once and made halves once.
+// Runs of 12 to 32 pages by sixteen rows: shorter ones are mostly what a block does once (its queries, its sums: two sequences of 150001 tokens, 2 heads,
+// 60 us with 4 pages, 45 with 8, 37 with 24), longer ones leave the last blocks of ragged sequences alone on the GPU; in between just under the 512 blocks that
+// the GPU holds.  By 128 rows about 2048 blocks, whose weights and sums for the splits are a tenth of a run of 24 pages.
 mdcnn_status plan_attend(const mdcnn_cache_desc& c, const mdcnn_attend_desc& a, int q_heads, int dtype, AttendJob& j, size_t* bytes) {
     j.pages = c.pages; j.heads = c.heads; j.group = q_heads / c.heads; j.dim = c.dim; j.pitch = mdcnn_cache_pitch(c.dim);
     j.n_seq = c.n_seq; j.max_pages = c.pages ? c.max_pages : 0;
@@ -245,8 +247,10 @@ mdcnn_status plan_attend(const mdcnn_cache_desc& c, const mdcnn_attend_desc& a, 
     long long most = std::min<long long>((a.max_len + (long long)MDCNN_PAGE_TOKENS - 1) / MDCNN_PAGE_TOKENS, c.max_pages);
     if (a.window) most = std::min<long long>(most, (a.window + (long long)j.max_new + 2 * MDCNN_PAGE_TOKENS - 2) / MDCNN_PAGE_TOKENS);
     most = std::max(most, 1ll);
-    j.run = j.tile_rows == kAttendRows ? (int)std::min(32ll, std::max(4ll, most * columns / 1024)) : (int)std::min(most, std::max(16ll, most * columns / 2048));
+    auto per = [&](long long blocks) { return (int)((most * columns + blocks - 1) / blocks); };
+    j.run = j.tile_rows == kAttendRows ? std::min(32, std::max(12, per(480))) : (int)std::min<long long>(most, std::max(8, per(2048)));
     j.splits = (int)((most + j.run - 1) / j.run);
+    j.run = (int)((most + j.splits - 1) / j.splits);                       // all alike
     if (columns >= (j.tile_rows == kAttendRows ? 2048 : 1024)) { j.splits = 1; j.run = 1 << 30; }
     if (columns * j.splits > 0x7fffffffll) return fail(MDCNN_ERR_SIZE, "cache_attend: too large");
     *bytes = j.splits > 1 ? (size_t)columns * j.splits * j.tile_rows * (8 + 4 * (size_t)j.pitch) + 256 : 0;
