@@ -10,8 +10,8 @@
 // exactly.  The scale of a page's keys is multiplied into the logits.  That of its values goes into the exponent,
 //   w = 2^(x + log2 vs - T),  T the row's largest x + log2 vs so far,
 // so that w is a half of full precision next to what counts most in this row, whatever the sizes of scales and values: sum w code / sum (w / vs)
-// is the result, 2^T sum (w / vs) the sum of the exponentials.  A page whose values are all zeros (vs below 2^-100) takes the scale of the
-// one before and weights of zero in the first sum.  (Scales of one sequence and head may lie 2^100 apart.)
+// is the result, 2^T sum (w / vs) the sum of the exponentials.  T is moved by pages that have values: those that are all zeros (vs below 2^-100) or not
+// numbers count in the second sum only, with the scale of the page before.  (Scales of one sequence and head may lie 2^100 apart.)
 #pragma once
 
 #include "ops_device.h"
@@ -95,8 +95,21 @@ __device__ __forceinline__ float factor_of(float logit, float ks) {
     return by < 1e-30f ? 1e-30f : by;
 }
 // T of a row is moved - and what has been summed faded - only where the weights of a lane add up to more than this (they have to be
-// halves): weights are made before anyone looks for a maximum, and on nearly all pages no one does.
-constexpr float kMuch = 16384.f;
+// halves, or finite where no values follow): weights are made before anyone looks for a maximum, and on nearly all pages no one does.
+constexpr float kMuch = 16384.f, kMuchNoValues = 18446744073709551616.f;
+
+// T of a row after a page whose largest x + log2 vs is `most` (minus infinity: the row sees none of it), and what the sums fade by.  The first page with
+// values sets it, whatever pages without values left (their sum is kept: no further down than that stays finite).
+struct NextTop {
+    float top, fade, fade_out;
+    __device__ __forceinline__ NextTop(float was, float most, bool moves, bool values, float& valued) {
+        const bool sets = values && valued == 0.f && most > -INFINITY;
+        top = !moves ? was : sets ? fmaxf(most, was - 100.f) : fmaxf(was, most);
+        fade = was == -INFINITY ? 1.f : exp2_fast(was - top);              // (nothing summed so far: nothing to fade)
+        fade_out = valued == 0.f ? 0.f : fade;                            // (nothing but zeros so far)
+        valued = sets ? 1.f : valued;
+    }
+};
 
 // Whether it holds in one of the lanes n and n + 32 (n, n + 16, n + 32, n + 48) that share a row.
 __device__ __forceinline__ bool row_of_two(bool here, int n) {

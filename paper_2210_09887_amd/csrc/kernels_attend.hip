@@ -77,6 +77,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
     const uint8_t* mask = j.mask ? j.mask + seq * j.mask_row : nullptr;
 
     float top = -INFINITY, sum = 0.f;                      // T and sum of this lane's row
+    float valued = 0.f;                                    // 1: the row has seen values (a mask would take two scalar registers, which are short)
     ValueScale val;
     float4v out[NV];
 #pragma unroll
@@ -174,18 +175,19 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
                 add = (part[0] + part[1]) + (part[2] + part[3]);
             };
             weigh();
-            bool moves = add > kMuch || (live && top == -INFINITY);
+            const bool values = !val.none && !val.bad;
+            bool moves = add > (values ? kMuch : kMuchNoValues) || (live && valued == 0.f);
             if (__any(moves)) {
                 moves = row_of_four(moves, n);
                 float m[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
                 for (int t = 4; t < 16; ++t) m[t % 4] = fmaxf(m[t % 4], x[t]);
-                const float most = max_over_32(max_over_16(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])))) * by + val.log, next_top = moves ? fmaxf(top, most) : top;
-                const float fade = top == -INFINITY ? 1.f : exp2_fast(top - next_top);           // (nothing summed so far: nothing to fade)
-                top = next_top;
-                sum *= fade;
+                const float most = max_over_32(max_over_16(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])))) * by + val.log;
+                const NextTop to(top, most, moves, values, valued);
+                top = to.top;
+                sum *= to.fade;
 #pragma unroll
-                for (int v = 0; v < NV; ++v) out[v] *= fade;
+                for (int v = 0; v < NV; ++v) out[v] *= to.fade_out;
                 weigh();
             }
             sum += add * val.inverse;

@@ -40,6 +40,8 @@ template <typename T, int DP, bool MASK>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (DP <= 64 ? 3 : DP <= 128 ? 2 : 1) : (DP == 32 ? 3 : DP <= 96 ? 2 : 1)) void k_attend_tiles(AttendJob j) {
     constexpr bool kTwo = sizeof(T) == 4;
     constexpr int NS = DP / 16, ND = DP / 32, NL = DP / 32;               // steps of channels, tiles of channels, 16-byte loads of a thread
+    constexpr int kHeld = DP > 192 ? 9 : NS;                              // steps of the queries in registers; the others lie in LDS behind the two stages
+    constexpr bool kAhead = DP <= 192;                                    // the next page's codes wait in registers while this one is worked on
     constexpr bool kAnew = DP > 128 || (DP == 64 && MASK);                // places in LDS are worked out anew for each page: registers are short
     using S = Stage<DP>;
     extern __shared__ __align__(16) unsigned char lds[];
@@ -59,7 +61,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (DP <= 64 ? 3 : DP <= 12
 
     const int row = r0 + 32 * wave + n, query = row / j.group;
     const bool live = row < s.rows;
-    half8 qh[NS], ql[kTwo ? NS : 1];
+    half8 qh[kHeld], ql[kTwo ? NS : 1];
+    half8* beyond = (half8*)(lds + 2 * S::kBytes) + threadIdx.x;
     int e;
     {
         const T* q = (const T*)j.q + (s.q0 + (live ? query : 0)) * j.q_token + (long long)(head * j.group + (live ? row % j.group : 0)) * j.q_head;
@@ -80,10 +83,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (DP <= 64 ? 3 : DP <= 12
             eight_of(q, 16 * st + 8 * half, live ? j.dim : 0, j.q_whole, f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float x = scaled(f[i], -e) * sign;
-                qh[st][i] = (_Float16)x;
-                if constexpr (kTwo) ql[st][i] = (_Float16)(x - (float)qh[st][i]);
+                f[i] = scaled(f[i], -e) * sign;
+                if constexpr (kTwo) ql[st][i] = (_Float16)(f[i] - (float)(_Float16)f[i]);
             }
+            half8 h;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = (_Float16)f[i];
+            if (st < kHeld) qh[st < kHeld ? st : 0] = h;
+            else beyond[(st - kHeld) * kThreads] = h;
         }
     }
     const float logit = scaled(fabsf(j.scale) * kLog2E, e);
@@ -95,6 +102,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (DP <= 64 ? 3 : DP <= 12
     const uint8_t* mask = MASK ? j.mask + seq * j.mask_row : nullptr;
 
     float top = -INFINITY, sum = 0.f;                      // T and sum of this lane's row
+    float valued = 0.f;                                    // 1: the row has seen values (a mask would take two scalar registers, which are short)
     ValueScale val;
     float16v out[ND];
 #pragma unroll
@@ -151,7 +159,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (DP <= 64 ? 3 : DP <= 12
     __syncthreads();
     for (int p = run.first; p < run.last; ++p) {
         const int after = page.at(p + 2);
-        if (p + 1 < run.last) load(next, p + 1);
+        if (kAhead && p + 1 < run.last) load(next, p + 1);
         const int pos = p * kPage;
         if (id >= 0 && pos < any_hi && pos + kPage > any_lo) {
             const float* beside = (const float*)(now + S::kKeys + S::kValues);
@@ -174,7 +182,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (DP <= 64 ? 3 : DP <= 12
             for (int i = 0; i < 2 * NS; ++i) {             // the two sums in turn, so that neither waits for itself; where registers are short one by one
                 const int st = DP <= 128 ? i / 2 : i % NS, a = DP <= 128 ? i % 2 : i / NS;
                 const half8 k = *(const half8*)(now + S::key_at(32 * a + place, 2 * st + half));
-                x[a] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qh[st], x[a], 0, 0, 0);
+                x[a] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, st < kHeld ? qh[st < kHeld ? st : 0] : beyond[(st - kHeld) * kThreads], x[a], 0, 0, 0);
                 if constexpr (kTwo) x[a] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, ql[st], x[a], 0, 0, 0);
             }
             // x[a][i] is token 32 half + 16 a + i
@@ -189,7 +197,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (DP <= 64 ? 3 : DP <= 12
             const float by = factor_of(logit, ks);
             val.next(vs);
             bool bad = false;                              // the row sees tokens whose scale is not a number
-            if (ks != ks || val.bad) {
+            if (__builtin_expect(ks != ks || val.bad, 0)) {
 #pragma unroll
                 for (int t = 0; t < 32; ++t) bad = bad || x[t / 16][t % 16] != -INFINITY;
                 bad = row_of_two(bad, n);
@@ -212,24 +220,25 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (DP <= 64 ? 3 : DP <= 12
                     add = (part[0] + part[1]) + (part[2] + part[3]);
                 };
                 weigh();
-                bool moves = add > kMuch || (live && top == -INFINITY);
-                if (__any(moves)) {
+                const bool values = !val.none && !val.bad;
+                bool moves = add > (values ? kMuch : kMuchNoValues) || (live && valued == 0.f);
+                if (__builtin_expect(__any(moves), 0)) {
                     moves = row_of_two(moves, n);
                     float m[4] = {x[0][0], x[0][1], x[0][2], x[0][3]};
 #pragma unroll
                     for (int t = 4; t < 32; ++t) m[t % 4] = fmaxf(m[t % 4], x[t / 16][t % 16]);
-                    const float most = max_over_32(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]))) * by + val.log, next_top = moves ? fmaxf(top, most) : top;
-                    const float fade = top == -INFINITY ? 1.f : exp2_fast(top - next_top);       // (nothing summed so far: nothing to fade)
-                    top = next_top;
-                    sum *= fade;
+                    const float most = max_over_32(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]))) * by + val.log;
+                    const NextTop to(top, most, moves, values, valued);
+                    top = to.top;
+                    sum *= to.fade;
 #pragma unroll
                     for (int d = 0; d < ND; ++d)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) out[d][i] *= fade;
+                        for (int i = 0; i < 16; ++i) out[d][i] *= to.fade_out;
                     weigh();
                 }
                 sum += add * val.inverse;
-                if (val.bad) {
+                if (__builtin_expect(val.bad, 0)) {
 #pragma unroll
                     for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -247,6 +256,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (DP <= 64 ? 3 : DP <= 12
                 sum = bad ? ks : sum;
             }
         }
+        if (!kAhead && p + 1 < run.last) load(next, p + 1);
         if (p + 1 < run.last) stage(then);
         page_over();
         _Float16* swap = now;
@@ -287,7 +297,7 @@ struct Tiles {
     }
     template <typename T, int DP, bool MASK>
     static hipError_t tiles(const AttendJob& j, hipStream_t st) {
-        constexpr int kLds = 2 * Stage<DP>::kBytes;
+        constexpr int kLds = 2 * Stage<DP>::kBytes + (DP > 192 ? (DP / 16 - 9) * kThreads * 16 : 0);
         const auto kern = k_attend_tiles<T, DP, MASK>;
         if (kLds > 64 * 1024) {
             const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);

@@ -334,3 +334,23 @@ def test_refusals():
     for bad in (lambda: w.c.attend(q[:, :3], t, s, n, 3, 10), lambda: w.c.attend(q, t, s, n, 3, 10, window=4), lambda: w.c.attend(q, t, s, n, 3, 10, float("nan"))):
         with pytest.raises(B.MdcnnError):
             bad()
+
+
+@pytest.mark.parametrize("counts", [[1], [150]], ids=str)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)      # (the results are smaller than halves resolve)
+@pytest.mark.parametrize("v_amp", [1e-12, 1.0, 1e12])
+def test_pages_of_zeros_first_last_and_between(v_amp, dtype, counts):
+    """Pages whose values are all zeros count in the sum of the exponentials and nowhere else, whatever comes before or after them."""
+    for zeros in ([0, 1, 2, 3, 4, 5], [0], [10, 11, 12, 13, 14, 15], [1, 5, 9], list(range(15)), list(range(16))):
+        w = World([1000], 1, 32, 19, v_amp=v_amp)
+        for k in zeros:
+            w.v.scale[w.table[0, k]] = 0
+            w.k.scale[w.table[0, k]] *= 2
+        w.c.v_scale.copy_(torch.from_numpy(w.v.scale))
+        w.c.k_scale.copy_(torch.from_numpy(w.k.scale))
+        w.queries(counts, 2, dtype)
+        if len(zeros) == 16:
+            out, lse = w.got(False)
+            assert not out.any() and bool(lse.isfinite().all())
+        else:
+            w.check(False)
