@@ -11,6 +11,8 @@
 //    whose joining would be most of a block's work, they are joined by a launch of their own.
 // Variances are sums of squares about a value of the channel itself, then about the means of ever larger sets: a mean that is large
 // beside the deviation costs no digits.  No atomics: sums are taken in one order.
+#include <type_traits>
+
 #include "ops_device.h"
 #include "ops_internal.h"
 
@@ -25,21 +27,29 @@ __device__ __forceinline__ long long at_pixel(const mdcnn_strides& s, int p, int
     return flat ? (long long)p * s.x : (long long)(p / W) * s.y + (long long)(p % W) * s.x;
 }
 
-__device__ __forceinline__ float act_of(float u, int act) {
-    if (act == MDCNN_ACT_SILU) return u * __builtin_amdgcn_rcpf(1.f + exp2_fast(-1.44269504f * u));
-    if (act == MDCNN_ACT_RELU) return u < 0.f ? 0.f : u;
+template <int ACT>
+__device__ __forceinline__ float act_of(float u) {
+    if (ACT == MDCNN_ACT_SILU) return u * __builtin_amdgcn_rcpf(1.f + exp2_fast(-1.44269504f * u));
+    if (ACT == MDCNN_ACT_RELU) return u < 0.f ? 0.f : u;
     return u;
 }
-// act'(u).  silu: s (1 + u (1 - s)) with 1 - s = e s, e = exp(-u), which keeps its digits where s is nearly one.
-__device__ __forceinline__ float slope_of(float u, int act) {
-    if (act == MDCNN_ACT_SILU) {
-        float e = exp2_fast(-1.44269504f * u);
-        e = e > 1e37f ? 1e37f : e;
-        const float s = __builtin_amdgcn_rcpf(1.f + e);
-        return s * (1.f + u * (e * s));
+// act'(u).  silu: s + u s (1 - s), s = 1 / (1 + exp(-u)); nothing of it overflows.
+template <int ACT>
+__device__ __forceinline__ float slope_of(float u) {
+    if (ACT == MDCNN_ACT_SILU) {
+        const float s = __builtin_amdgcn_rcpf(1.f + exp2_fast(-1.44269504f * u));
+        return __builtin_fmaf(u * s, 1.f - s, s);
     }
-    if (act == MDCNN_ACT_RELU) return u > 0.f ? 1.f : u == u ? 0.f : u;
+    if (ACT == MDCNN_ACT_RELU) return u > 0.f ? 1.f : u == u ? 0.f : u;
     return 1.f;
+}
+
+// f with the activation as a constant: one decision to a loop instead of one to a value.
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F&& f) {
+    if (act == MDCNN_ACT_SILU) f(std::integral_constant<int, MDCNN_ACT_SILU>());
+    else if (act == MDCNN_ACT_RELU) f(std::integral_constant<int, MDCNN_ACT_RELU>());
+    else f(std::integral_constant<int, MDCNN_ACT_NONE>());
 }
 
 // Block of a chunked launch: image, chunk, slice of channels and the thread's place in it.
@@ -63,53 +73,69 @@ __device__ __forceinline__ Place place_of(const NormJob& j, unsigned blk) {
 
 __device__ __forceinline__ int pow2_over(int n) { return n >= 64 ? 64 : n <= 1 ? 1 : 1 << (32 - __clz(n - 1)); }
 
-// Joins per channel the (mean, squares) that the rows of threads left in s[row][c], each over the pixels r0 + row,
-// r0 + row + row_lanes ..; result in s[0][c].
-__device__ __forceinline__ void join_rows(float2* s, int nc, int row_lanes, int pixels) {
-    __syncthreads();
-    if (row_lanes > 1)
-        for (int c = threadIdx.x; c < nc; c += blockDim.x) {
-            float n = 0.f, mean = 0.f, sq = 0.f;
-            for (int r = 0; r < row_lanes && r < pixels; ++r) {
-                const float2 v = s[r * nc + c];
-                const float k = (float)((pixels - r + row_lanes - 1) / row_lanes), d = v.x - mean, f = k / (n + k);
-                mean += d * f;
-                sq += v.y + d * d * n * f;
-                n += k;
-            }
-            s[c] = make_float2(mean, sq);
-        }
-    __syncthreads();
+// Lanes to a group: as many as the block has for all its groups, no more than there are elements.
+__device__ __forceinline__ int lanes_for(int groups, int elements) {
+    int w = pow2_over(elements);
+    while (w > 1 && w * groups > (int)blockDim.x) w >>= 1;
+    return w;
 }
-__device__ __forceinline__ void add_rows(float2* s, int nc, int row_lanes) {
-    __syncthreads();
-    if (row_lanes > 1)
-        for (int c = threadIdx.x; c < nc; c += blockDim.x) {
-            float a = 0.f, b = 0.f;
-            for (int r = 0; r < row_lanes; ++r) { const float2 v = s[r * nc + c]; a += v.x; b += v.y; }
-            s[c] = make_float2(a, b);
-        }
-    __syncthreads();
-}
-// Per group of the slice, from the channels' s[c]: (mean, squares about it), each channel over `pixels` pixels.
+
+// Per group of the slice, from what the rows of threads left in s[row][c] - mean and squares about it of a channel's pixels row, row + row_lanes .. - the
+// same over all its channels and pixels: out(group, mean, squares).
 template <typename F>
-__device__ __forceinline__ void join_channels(const float2* s, int nc, int cpg, int pixels, F&& out) {
-    const int w = pow2_over(cpg), lane = threadIdx.x % w;
-    for (int g = threadIdx.x / w; g * cpg < nc; g += blockDim.x / w) {
-        float m = 0.f;
-        for (int c = lane; c < cpg; c += w) m += s[g * cpg + c].x;
-        m = sum_lanes(m, w) / (float)cpg;
-        float sq = 0.f;
-        for (int c = lane; c < cpg; c += w) { const float2 v = s[g * cpg + c]; sq += v.y + (float)pixels * (v.x - m) * (v.x - m); }
+__device__ __forceinline__ void join_groups(const float2* s, int nc, int cpg, int row_lanes, int pixels, F&& out) {
+    __syncthreads();
+    const int groups = nc / cpg, rows = min(row_lanes, pixels), w = lanes_for(groups, rows * cpg), lane = threadIdx.x % w;
+    const int whole = (pixels + row_lanes - 1) / row_lanes, more = pixels % row_lanes, dr = w / cpg, dc = w % cpg;
+    const float inv = 1.f / ((float)pixels * (float)cpg);
+    for (int g = threadIdx.x / w; g < groups; g += blockDim.x / w) {
+        auto each = [&](auto&& f) {
+#pragma unroll 4
+            for (int r = lane / cpg, c = lane % cpg; r < rows;) {
+                f(s[r * nc + g * cpg + c], (float)(!more || r < more ? whole : whole - 1));
+                r += dr;
+                c += dc;
+                if (c >= cpg) { c -= cpg; ++r; }
+            }
+        };
+        float m = 0.f, sq = 0.f;
+        each([&](float2 v, float k) { m = __builtin_fmaf(v.x, k, m); });
+        m = sum_lanes(m, w) * inv;
+        each([&](float2 v, float k) { sq += __builtin_fmaf((v.x - m) * (v.x - m), k, v.y); });
         sq = sum_lanes(sq, w);
         if (lane == 0) out(g, m, sq);
     }
 }
+// Sums of the rows of threads per channel: in s[0][c].
+__device__ __forceinline__ void add_rows(float2* s, int nc, int row_lanes) {
+    __syncthreads();
+    if (row_lanes < 2) return;
+    // sets of threads over the channels each take every sets-th row, then the first takes the sets
+    const int sets = max(1, min(row_lanes, (int)blockDim.x / nc));
+    const int set = threadIdx.x / nc;
+    if (set < sets)
+        for (int c = threadIdx.x - set * nc; c < nc; c += sets > 1 ? nc : blockDim.x) {
+            float a = 0.f, b = 0.f;
+#pragma unroll 4
+            for (int r = set; r < row_lanes; r += sets) { const float2 v = s[r * nc + c]; a += v.x; b += v.y; }
+            s[set * nc + c] = make_float2(a, b);           // (a row that only this thread reads)
+        }
+    __syncthreads();
+    if (sets > 1) {
+        if (set == 0) {
+            float a = 0.f, b = 0.f;
+            for (int r = 0; r < sets; ++r) { const float2 v = s[r * nc + threadIdx.x]; a += v.x; b += v.y; }
+            s[threadIdx.x] = make_float2(a, b);
+        }
+        __syncthreads();
+    }
+}
 template <typename F>
 __device__ __forceinline__ void add_channels(const float2* s, int nc, int cpg, F&& out) {
-    const int w = pow2_over(cpg), lane = threadIdx.x % w;
-    for (int g = threadIdx.x / w; g * cpg < nc; g += blockDim.x / w) {
+    const int groups = nc / cpg, w = lanes_for(groups, cpg), lane = threadIdx.x % w;
+    for (int g = threadIdx.x / w; g < groups; g += blockDim.x / w) {
         float a = 0.f, b = 0.f;
+#pragma unroll 4
         for (int c = lane; c < cpg; c += w) { const float2 v = s[g * cpg + c]; a += v.x; b += v.y; }
         a = sum_lanes(a, w);
         b = sum_lanes(b, w);
@@ -120,10 +146,11 @@ __device__ __forceinline__ void add_channels(const float2* s, int nc, int cpg, F
 __device__ __forceinline__ float2 join_chunks(const NormJob& j, int n, int g, int lane, int w) {
     const float2* p = (const float2*)j.part + ((size_t)n * j.chunks) * j.groups + g;
     const float whole = (float)j.rows, last = (float)(j.P - (j.chunks - 1) * j.rows), inv = 1.f / (float)j.P;
-    float m = 0.f;
+    float m = 0.f, sq = 0.f;
+#pragma unroll 4
     for (int k = lane; k < j.chunks; k += w) m += p[(size_t)k * j.groups].x * ((k == j.chunks - 1 ? last : whole) * inv);
     m = sum_lanes(m, w);
-    float sq = 0.f;
+#pragma unroll 4
     for (int k = lane; k < j.chunks; k += w) {
         const float2 v = p[(size_t)k * j.groups];
         sq += v.y + (k == j.chunks - 1 ? last : whole) * (float)j.cpg * (v.x - m) * (v.x - m);
@@ -134,55 +161,88 @@ __device__ __forceinline__ float2 join_chunks(const NormJob& j, int n, int g, in
 __device__ __forceinline__ float2 add_chunks(const NormJob& j, int n, int g, int lane, int w) {
     const float2* p = (const float2*)j.part + ((size_t)n * j.chunks) * j.groups + g;
     float a = 0.f, b = 0.f;
+#pragma unroll 4
     for (int k = lane; k < j.chunks; k += w) { const float2 v = p[(size_t)k * j.groups]; a += v.x; b += v.y; }
     return make_float2(sum_lanes(a, w) * j.inv_count, sum_lanes(b, w) * j.inv_count);
 }
 
-// What of a vector of channels does not change from pixel to pixel.
+// Groups of the channels c .. c + VEC - 1, counted from `first`, one division for all.
+template <int VEC, typename F>
+__device__ __forceinline__ void each_group(const NormJob& j, int c, int first, F&& f) {
+    int g = c / j.cpg, in = c - g * j.cpg;
+    g -= first;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        f(i, g);
+        if (++in == j.cpg) { in = 0; ++g; }
+    }
+}
+
+// What of a vector of channels does not change from pixel to pixel: y = act((x - mean) scale + beta), scale = gamma rstd.
 template <int VEC>
 struct Channels {
     float mean[VEC], scale[VEC], beta[VEC];
-    __device__ __forceinline__ void load(const NormJob& j, int c, const float* mean_of, const float* rstd_of, int first_group) {
+    __device__ __forceinline__ void load_affine(const NormJob& j, int c) {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            const int g = (c + i) / j.cpg - first_group;
-            mean[i] = mean_of[g];
-            scale[i] = rstd_of[g] * (j.gamma ? j.gamma[c + i] : 1.f);
+            scale[i] = j.gamma ? j.gamma[c + i] : 1.f;
             beta[i] = j.beta ? j.beta[c + i] : 0.f;
         }
     }
-    template <typename T>
-    __device__ __forceinline__ Pack<T, VEC> apply(const Pack<T, VEC>& x, int act) const {
+    __device__ __forceinline__ void load_stats(const NormJob& j, int c, const float* mean_of, const float* rstd_of, int first_group) {
+        each_group<VEC>(j, c, first_group, [&](int i, int g) { mean[i] = mean_of[g]; scale[i] *= rstd_of[g]; });
+    }
+    template <int ACT, typename T>
+    __device__ __forceinline__ Pack<T, VEC> apply(const Pack<T, VEC>& x) const {
         float f[VEC];
         unpack(x, f);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) f[i] = act_of((f[i] - mean[i]) * scale[i] + beta[i], act);
+        for (int i = 0; i < VEC; ++i) f[i] = act_of<ACT>(__builtin_fmaf(f[i] - mean[i], scale[i], beta[i]));
         return pack<T, VEC>(f);
     }
 };
+// The same for gradients, with du = act'(u) dy and d = x - mean:
+//   dx = scale du - rstd m1 - rstd^2 m2' d,   m2' = mean(gamma du d)
 template <int VEC>
 struct GradChannels {
-    float mean[VEC], rstd[VEC], gamma[VEC], beta[VEC];
+    float mean[VEC], scale[VEC], beta[VEC];
     __device__ __forceinline__ void load(const NormJob& j, int n, int c) {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const size_t g = (size_t)n * j.groups + (c + i) / j.cpg;
-            mean[i] = j.mean[g];
-            rstd[i] = j.rstd[g];
-            gamma[i] = j.gamma ? j.gamma[c + i] : 1.f;
+        each_group<VEC>(j, c, 0, [&](int i, int g) {
+            const size_t at = (size_t)n * j.groups + g;
+            mean[i] = j.mean[at];
+            scale[i] = j.rstd[at] * (j.gamma ? j.gamma[c + i] : 1.f);
             beta[i] = j.beta ? j.beta[c + i] : 0.f;
-        }
+        });
     }
-    // du = act'(u) dy and z of every channel
-    template <typename T>
-    __device__ __forceinline__ void of(const Pack<T, VEC>& x, const Pack<T, VEC>& dy, int act, float (&du)[VEC], float (&z)[VEC]) const {
-        unpack(x, z);
+    template <int ACT, typename T>
+    __device__ __forceinline__ void of(const Pack<T, VEC>& x, const Pack<T, VEC>& dy, float (&du)[VEC], float (&d)[VEC]) const {
+        unpack(x, d);
         unpack(dy, du);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            z[i] = (z[i] - mean[i]) * rstd[i];
-            if (act != MDCNN_ACT_NONE) du[i] *= slope_of(z[i] * gamma[i] + beta[i], act);
+            d[i] -= mean[i];
+            if (ACT != MDCNN_ACT_NONE) du[i] *= slope_of<ACT>(__builtin_fmaf(d[i], scale[i], beta[i]));
         }
+    }
+};
+// The two terms that a group's sums take from its gradients.
+template <int VEC>
+struct GradTerms {
+    float one[VEC], two[VEC];
+    __device__ __forceinline__ void load(const NormJob& j, int n, int c, const float2* sums, int first_group) {
+        each_group<VEC>(j, c, first_group, [&](int i, int g) {
+            const float r = j.rstd[(size_t)n * j.groups + first_group + g];
+            const float2 v = sums[g];
+            one[i] = r * v.x;
+            two[i] = r * v.y;
+        });
+    }
+    template <typename T>
+    __device__ __forceinline__ Pack<T, VEC> gradient(const GradChannels<VEC>& ch, const float (&du)[VEC], const float (&d)[VEC]) const {
+        float f[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) f[i] = __builtin_fmaf(du[i], ch.scale[i], -__builtin_fmaf(d[i], two[i], one[i]));
+        return pack<T, VEC>(f);
     }
 };
 
@@ -207,7 +267,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_stats(NormJob j) {
                 for (int i = 0; i < VEC; ++i) {
                     const float d = f[i] - pivot[i];
                     s1[i] += d;
-                    s2[i] += d * d;
+                    s2[i] = __builtin_fmaf(d, d, s2[i]);
                 }
             }
             const int k = first < p.r1 ? (p.r1 - first + j.row_lanes - 1) / j.row_lanes : 1;
@@ -218,9 +278,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_stats(NormJob j) {
                 s[p.row * p.nc + c + i] = make_float2(pivot[i] + d, sq < 0.f ? 0.f : sq);
             }
         }
-    join_rows(s, p.nc, j.row_lanes, p.r1 - p.r0);
     float2* out = (float2*)j.part + ((size_t)p.n * j.chunks + p.chunk) * j.groups + p.c0 / j.cpg;
-    join_channels(s, p.nc, j.cpg, p.r1 - p.r0, [&](int g, float m, float sq) { out[g] = make_float2(m, sq); });
+    join_groups(s, p.nc, j.cpg, j.row_lanes, p.r1 - p.r0, [&](int g, float m, float sq) { out[g] = make_float2(m, sq); });
 }
 
 __global__ __launch_bounds__(kThreads) void k_norm_join(NormJob j) {
@@ -236,10 +295,10 @@ __global__ __launch_bounds__(kThreads) void k_norm_apply(NormJob j) {
     extern __shared__ float2 s[];
     float* mean = (float*)s;
     float* rstd = mean + j.slice / j.cpg;
-    const Place p = place_of(j, blockIdx.x);
+    const Place p = place_of(j, gridDim.x - 1 - blockIdx.x);              // what was read last comes first: the caches hold that
     const int g0 = p.c0 / j.cpg;
     if (j.chunks <= kJoinHere) {
-        const int w = pow2_over(j.chunks), lane = threadIdx.x % w;
+        const int w = lanes_for(p.nc / j.cpg, j.chunks), lane = threadIdx.x % w;
         for (int g = threadIdx.x / w; g * j.cpg < p.nc; g += kThreads / w) {
             const float2 v = join_chunks(j, p.n, g0 + g, lane, w);
             if (lane == 0) {
@@ -260,10 +319,13 @@ __global__ __launch_bounds__(kThreads) void k_norm_apply(NormJob j) {
     T* y = (T*)j.y + (long long)p.n * j.ys.n;
     for (int c = p.c0 + p.lane * VEC; c < p.c0 + p.nc; c += j.lanes * VEC) {
         Channels<VEC> ch;
-        ch.load(j, c, mean, rstd, g0);
+        ch.load_affine(j, c);
+        ch.load_stats(j, c, mean, rstd, g0);
+        with_act(j.act, [&](auto act) {
 #pragma unroll 4
-        for (int r = p.r0 + p.row; r < p.r1; r += j.row_lanes)
-            *(Pack<T, VEC>*)(y + at_pixel(j.ys, r, j.W, j.flat) + c) = ch.apply(*(const Pack<T, VEC>*)(x + at_pixel(j.xs, r, j.W, j.flat) + c), j.act);
+            for (int r = p.r0 + p.row; r < p.r1; r += j.row_lanes)
+                *(Pack<T, VEC>*)(y + at_pixel(j.ys, r, j.W, j.flat) + c) = ch.template apply<act()>(*(const Pack<T, VEC>*)(x + at_pixel(j.xs, r, j.W, j.flat) + c));
+        });
     }
 }
 
@@ -280,7 +342,9 @@ __global__ __launch_bounds__(VEC == 8 ? 512 : 1024) void k_norm_held(NormJob j) 
 #pragma unroll
     for (int q = 0; q < HELD; ++q)
         if (q < k) v[q] = *(const Pack<T, VEC>*)(x + at_pixel(j.xs, p.row + q * j.row_lanes, j.W, j.flat) + c);
+    Channels<VEC> ch;
     if (on) {
+        ch.load_affine(j, c);
         float m[VEC], sq[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; ++i) m[i] = sq[i] = 0.f;
@@ -301,17 +365,16 @@ __global__ __launch_bounds__(VEC == 8 ? 512 : 1024) void k_norm_held(NormJob j) 
                 float f[VEC];
                 unpack(v[q], f);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) sq[i] += (f[i] - m[i]) * (f[i] - m[i]);
+                for (int i = 0; i < VEC; ++i) sq[i] = __builtin_fmaf(f[i] - m[i], f[i] - m[i], sq[i]);
             }
 #pragma unroll
         for (int i = 0; i < VEC; ++i) s[p.row * p.nc + p.lane * VEC + i] = make_float2(m[i], sq[i]);
     }
-    join_rows(s, p.nc, j.row_lanes, j.P);
     const int g0 = p.c0 / j.cpg;
     // behind the channels: mean and rstd of the groups
     float* mean = (float*)(s + (size_t)j.row_lanes * p.nc);
     float* rstd = mean + p.nc / j.cpg;
-    join_channels(s, p.nc, j.cpg, j.P, [&](int g, float m, float sq) {
+    join_groups(s, p.nc, j.cpg, j.row_lanes, j.P, [&](int g, float m, float sq) {
         const float r = 1.f / sqrtf(sq * j.inv_count + j.eps);
         mean[g] = m;
         rstd[g] = r;
@@ -321,11 +384,12 @@ __global__ __launch_bounds__(VEC == 8 ? 512 : 1024) void k_norm_held(NormJob j) 
     __syncthreads();
     if (!on) return;
     T* y = (T*)j.y + (long long)p.n * j.ys.n;
-    Channels<VEC> ch;
-    ch.load(j, c, mean, rstd, g0);
+    ch.load_stats(j, c, mean, rstd, g0);
+    with_act(j.act, [&](auto act) {
 #pragma unroll
-    for (int q = 0; q < HELD; ++q)
-        if (q < k) *(Pack<T, VEC>*)(y + at_pixel(j.ys, p.row + q * j.row_lanes, j.W, j.flat) + c) = ch.apply(v[q], j.act);
+        for (int q = 0; q < HELD; ++q)
+            if (q < k) *(Pack<T, VEC>*)(y + at_pixel(j.ys, p.row + q * j.row_lanes, j.W, j.flat) + c) = ch.template apply<act()>(v[q]);
+    });
 }
 
 // ---- gradients --------------------------------------------------------------------------------------------------------
@@ -342,26 +406,29 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad_sums(NormJob j) {
             float s1[VEC], s2[VEC];
 #pragma unroll
             for (int i = 0; i < VEC; ++i) s1[i] = s2[i] = 0.f;
-#pragma unroll 2
-            for (int r = p.r0 + p.row; r < p.r1; r += j.row_lanes) {
-                float du[VEC], z[VEC];
-                ch.of(*(const Pack<T, VEC>*)(x + at_pixel(j.xs, r, j.W, j.flat) + c), *(const Pack<T, VEC>*)(dy + at_pixel(j.ds, r, j.W, j.flat) + c), j.act, du, z);
+            with_act(j.act, [&](auto act) {
+#pragma unroll 4
+                for (int r = p.r0 + p.row; r < p.r1; r += j.row_lanes) {
+                    float du[VEC], d[VEC];
+                    ch.template of<act()>(*(const Pack<T, VEC>*)(x + at_pixel(j.xs, r, j.W, j.flat) + c), *(const Pack<T, VEC>*)(dy + at_pixel(j.ds, r, j.W, j.flat) + c), du, d);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    s1[i] += du[i];
-                    s2[i] += du[i] * z[i];
+                    for (int i = 0; i < VEC; ++i) {
+                        s1[i] += du[i];
+                        s2[i] = __builtin_fmaf(du[i], d[i], s2[i]);
+                    }
                 }
-            }
+            });
 #pragma unroll
             for (int i = 0; i < VEC; ++i) s[p.row * p.nc + c - p.c0 + i] = make_float2(s1[i], s2[i]);
         }
     add_rows(s, p.nc, j.row_lanes);
     float2* cpart = (float2*)j.cpart + ((size_t)p.n * j.chunks + p.chunk) * j.C + p.c0;
     for (int c = threadIdx.x; c < p.nc; c += kThreads) {
-        float2 v = s[c];
+        const float r = j.rstd[(size_t)p.n * j.groups + (p.c0 + c) / j.cpg];
+        const float2 v = make_float2(s[c].x, s[c].y * r);  // of du and of du z
         cpart[c] = v;
         const float gamma = j.gamma ? j.gamma[p.c0 + c] : 1.f;
-        s[c] = make_float2(v.x * gamma, v.y * gamma);
+        s[c] = make_float2(v.x * gamma, v.y * gamma * r);
     }
     __syncthreads();
     float2* out = (float2*)j.part + ((size_t)p.n * j.chunks + p.chunk) * j.groups + p.c0 / j.cpg;
@@ -403,14 +470,6 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad_channels(NormJob j) {
     channel_gradients(j, blockIdx.x, s);
 }
 
-template <int VEC, typename T>
-__device__ __forceinline__ Pack<T, VEC> grad_of(const GradChannels<VEC>& ch, const float (&du)[VEC], const float (&z)[VEC], const float (&m1)[VEC], const float (&m2)[VEC]) {
-    float f[VEC];
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) f[i] = ch.rstd[i] * (du[i] * ch.gamma[i] - m1[i] - z[i] * m2[i]);
-    return pack<T, VEC>(f);
-}
-
 template <typename T, int VEC>
 __global__ __launch_bounds__(kThreads) void k_norm_grad_apply(NormJob j) {
     extern __shared__ float2 s[];
@@ -419,10 +478,10 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad_apply(NormJob j) {
         channel_gradients(j, blockIdx.x, s);
         return;
     }
-    const Place p = place_of(j, blockIdx.x - columns);
+    const Place p = place_of(j, gridDim.x - 1 - blockIdx.x);              // what was read last comes first: the caches hold that
     const int g0 = p.c0 / j.cpg;
     if (j.chunks <= kJoinHere) {
-        const int w = pow2_over(j.chunks), lane = threadIdx.x % w;
+        const int w = lanes_for(p.nc / j.cpg, j.chunks), lane = threadIdx.x % w;
         for (int g = threadIdx.x / w; g * j.cpg < p.nc; g += kThreads / w) {
             const float2 v = add_chunks(j, p.n, g0 + g, lane, w);
             if (lane == 0) s[g] = v;
@@ -438,19 +497,16 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad_apply(NormJob j) {
     for (int c = p.c0 + p.lane * VEC; c < p.c0 + p.nc; c += j.lanes * VEC) {
         GradChannels<VEC> ch;
         ch.load(j, p.n, c);
-        float m1[VEC], m2[VEC];
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const float2 v = s[(c + i) / j.cpg - g0];
-            m1[i] = v.x;
-            m2[i] = v.y;
-        }
+        GradTerms<VEC> terms;
+        terms.load(j, p.n, c, s, g0);
+        with_act(j.act, [&](auto act) {
 #pragma unroll 2
-        for (int r = p.r0 + p.row; r < p.r1; r += j.row_lanes) {
-            float du[VEC], z[VEC];
-            ch.of(*(const Pack<T, VEC>*)(x + at_pixel(j.xs, r, j.W, j.flat) + c), *(const Pack<T, VEC>*)(dy + at_pixel(j.ds, r, j.W, j.flat) + c), j.act, du, z);
-            *(Pack<T, VEC>*)(dx + at_pixel(j.ys, r, j.W, j.flat) + c) = grad_of<VEC, T>(ch, du, z, m1, m2);
-        }
+            for (int r = p.r0 + p.row; r < p.r1; r += j.row_lanes) {
+                float du[VEC], d[VEC];
+                ch.template of<act()>(*(const Pack<T, VEC>*)(x + at_pixel(j.xs, r, j.W, j.flat) + c), *(const Pack<T, VEC>*)(dy + at_pixel(j.ds, r, j.W, j.flat) + c), du, d);
+                *(Pack<T, VEC>*)(dx + at_pixel(j.ys, r, j.W, j.flat) + c) = terms.template gradient<T>(ch, du, d);
+            }
+        });
     }
 }
 
@@ -476,23 +532,26 @@ __global__ __launch_bounds__(VEC == 8 ? 512 : 1024) void k_norm_grad_held(NormJo
         float s1[VEC], s2[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; ++i) s1[i] = s2[i] = 0.f;
+        with_act(j.act, [&](auto act) {
 #pragma unroll
-        for (int q = 0; q < HELD; ++q)
-            if (q < k) {
-                float du[VEC], z[VEC];
-                ch.of(v[q], w[q], j.act, du, z);
+            for (int q = 0; q < HELD; ++q)
+                if (q < k) {
+                    float du[VEC], d[VEC];
+                    ch.template of<act()>(v[q], w[q], du, d);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    s1[i] += du[i];
-                    s2[i] += du[i] * z[i];
+                    for (int i = 0; i < VEC; ++i) {
+                        s1[i] += du[i];
+                        s2[i] = __builtin_fmaf(du[i], d[i], s2[i]);
+                    }
                 }
-            }
+        });
 #pragma unroll
         for (int i = 0; i < VEC; ++i) s[p.row * p.nc + p.lane * VEC + i] = make_float2(s1[i], s2[i]);
     }
     add_rows(s, p.nc, j.row_lanes);
     for (int q = threadIdx.x; q < p.nc; q += blockDim.x) {
-        const float2 t = s[q];
+        const float r = j.rstd[(size_t)p.n * j.groups + (p.c0 + q) / j.cpg];
+        const float2 t = make_float2(s[q].x, s[q].y * r);
         if (j.N == 1) {                                    // this block's sums are the gradients
             j.dbeta[p.c0 + q] = t.x;
             j.dgamma[p.c0 + q] = t.y;
@@ -500,7 +559,7 @@ __global__ __launch_bounds__(VEC == 8 ? 512 : 1024) void k_norm_grad_held(NormJo
             ((float2*)j.cpart)[(size_t)p.n * j.C + p.c0 + q] = t;
         }
         const float gamma = j.gamma ? j.gamma[p.c0 + q] : 1.f;
-        s[q] = make_float2(t.x * gamma, t.y * gamma);
+        s[q] = make_float2(t.x * gamma, t.y * gamma * r);
     }
     __syncthreads();
     float2* sums = s + (size_t)j.row_lanes * p.nc;
@@ -508,20 +567,17 @@ __global__ __launch_bounds__(VEC == 8 ? 512 : 1024) void k_norm_grad_held(NormJo
     __syncthreads();
     if (!on) return;
     T* dx = (T*)j.y + (long long)p.n * j.ys.n;
-    float m1[VEC], m2[VEC];
+    GradTerms<VEC> terms;
+    terms.load(j, p.n, c, sums, p.c0 / j.cpg);
+    with_act(j.act, [&](auto act) {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-        const float2 t = sums[(c + i) / j.cpg - p.c0 / j.cpg];
-        m1[i] = t.x;
-        m2[i] = t.y;
-    }
-#pragma unroll
-    for (int q = 0; q < HELD; ++q)
-        if (q < k) {
-            float du[VEC], z[VEC];
-            ch.of(v[q], w[q], j.act, du, z);
-            *(Pack<T, VEC>*)(dx + at_pixel(j.ys, p.row + q * j.row_lanes, j.W, j.flat) + c) = grad_of<VEC, T>(ch, du, z, m1, m2);
-        }
+        for (int q = 0; q < HELD; ++q)
+            if (q < k) {
+                float du[VEC], d[VEC];
+                ch.template of<act()>(v[q], w[q], du, d);
+                *(Pack<T, VEC>*)(dx + at_pixel(j.ys, p.row + q * j.row_lanes, j.W, j.flat) + c) = terms.template gradient<T>(ch, du, d);
+            }
+    });
 }
 
 // LDS: a float2 per row of threads and channel, behind them two floats per group.

@@ -85,14 +85,14 @@ int plan_norm(const mdcnn_group_norm_desc& d, bool backward, int vec, NormJob& j
             }
         }
     }
-    // In chunks: up to 128 vectors beside one another, so that few of 256 threads are left over; 16 vectors to a thread, fewer
+    // In chunks: up to 128 vectors beside one another, so that few of 256 threads are left over; 32 vectors to a thread, fewer
     // (down to 4) where that leaves less than four blocks to a compute unit.
     j.slice = std::min(j.C, unit * std::max(1, 128 * vec / unit));
     j.slices = (j.C + j.slice - 1) / j.slice;
     j.lanes = std::min(j.slice / vec, kNormThreads);
     j.row_lanes = kNormThreads / j.lanes;
     const long long per_row = (long long)images * j.slices;
-    long long deep = 16;
+    long long deep = 32;
     while (deep > 4 && per_row * ((j.P + deep * j.row_lanes - 1) / (deep * j.row_lanes)) < 1024) deep /= 2;
     j.rows = (int)std::min<long long>(j.P, deep * j.row_lanes);
     j.chunks = (j.P + j.rows - 1) / j.rows;
