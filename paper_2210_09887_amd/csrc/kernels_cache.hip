@@ -51,41 +51,75 @@ __device__ __forceinline__ unsigned block_max(unsigned v, unsigned* s) {
     return v;
 }
 
-__device__ __forceinline__ int code_of(float x, float scale) {
+// Codes of four values, a byte each: the quotients rounded to nearest even.  A product with the reciprocal is off by 2^-15 at most: only where that
+// could decide between two codes are the divisions made.
+__device__ __forceinline__ unsigned codes_of(const float (&x)[4], float scale, float inverse) {
     if (!(scale > 0.f)) return 0;                                            // all zeros, or not finite
-    return (int)fminf(fmaxf(rintf(x / scale), -127.f), 127.f);
+    float q[4], near = inverse < 3e38f ? 0.f : 1.f;                          // (a scale below 2^-128 has no finite reciprocal)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float y = x[i] * inverse;
+        q[i] = rintf(y);
+        near = fmaxf(near, fabsf(y - q[i]));
+    }
+    if (!(near < 0.4999f))
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = rintf(x[i] / scale);
+    unsigned word = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) word |= ((unsigned)(int)fminf(fmaxf(q[i], -127.f), 127.f) & 0xffu) << (8 * i);
+    return word;
+}
+// Old codes of a page whose scale has grown.
+__device__ __forceinline__ unsigned smaller(unsigned word, float ratio) {
+    unsigned r = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r |= ((unsigned)(int)rintf((float)(int8_t)(word >> (8 * i)) * ratio) & 0xffu) << (8 * i);
+    return r;
 }
 
-// Channels VEC beside one another; the tokens' values pass through LDS as floats, so that they are read once.
+// A thread has VEC channels of four tokens (of four more every pass) in registers from the one read to the codes.  Values are turned in LDS, so that
+// they leave as 16 tokens of a channel.
 template <typename T, int VEC>
 __global__ __launch_bounds__(kThreads) void k_cache_store(CacheJob j) {
-    extern __shared__ float vals[];                                          // [tokens][dim + 1]
+    constexpr int kPasses = 16 / VEC < 1 ? 1 : 16 / VEC;                     // 256 channels
+    extern __shared__ __align__(16) unsigned turned[];                       // values: [dim][kPage / 4 + 4], in words of four tokens
+    constexpr int kRow = kPage / 4 + 4;
     __shared__ unsigned s_max[4];
     PageOf p;
     if (!p.find(j) || p.page < 0) return;
     const CacheMap& m = p.is_v ? j.v : j.k;
     const int base = p.slot * kPage;                                         // position of the page's first token
     const int t0 = max(p.first - base, 0), t1 = min(p.count - (base - p.first), kPage);   // its tokens that are new
-    const long long row0 = (long long)p.row + (base - p.first);
-    const T* x = (const T*)m.x + p.head * m.x_head;
-    const int vecs = j.dim / VEC, n = (t1 - t0) * vecs, pitch = j.dim + 1;
+    const T* x = (const T*)m.x + p.head * m.x_head + ((long long)p.row + (base - p.first)) * m.x_token;
+    const int vecs = j.dim / VEC, sets = kThreads / vecs, set = threadIdx.x / vecs, c = (threadIdx.x - set * vecs) * VEC;
+    Pack<T, VEC> v[kPasses][4];
     unsigned top = 0;
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        const int t = i / vecs, c = (i % vecs) * VEC;
-        float f[VEC];
-        unpack(*(const Pack<T, VEC>*)(x + (row0 + t0 + t) * m.x_token + c), f);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            vals[t * pitch + c + e] = f[e];
-            top = max(top, __float_as_uint(f[e]) & 0x7fffffffu);
+    for (int q = 0; q < kPasses; ++q)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = 4 * (set + q * sets) + i;
+            if (set < sets && t >= t0 && t < t1) v[q][i] = *(const Pack<T, VEC>*)(x + t * m.x_token + c);
         }
-    }
-    top = block_max(top, s_max);
+#pragma unroll
+    for (int q = 0; q < kPasses; ++q)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = 4 * (set + q * sets) + i;
+            if (set < sets && t >= t0 && t < t1) {
+                float f[VEC];
+                unpack(v[q][i], f);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) top = max(top, __float_as_uint(f[e]) & 0x7fffffffu);
+            }
+        }
     float* scale_at = (p.is_v ? j.v_scale : j.k_scale) + p.page * j.heads + p.head;
+    const float old = t0 > 0 ? *scale_at : 0.f;
+    top = block_max(top, s_max);                                             // (behind it, everyone has read the old scale)
     const float need = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : __uint_as_float(top) / 127.f;
     float scale = need, ratio = 1.f;
     if (t0 > 0) {                                                            // the page holds t0 tokens already
-        const float old = *scale_at;
         if (need <= old) {
             scale = old;
         } else {
@@ -93,86 +127,144 @@ __global__ __launch_bounds__(kThreads) void k_cache_store(CacheJob j) {
             ratio = scale > 0.f ? old / scale : 0.f;
         }
     }
-    __syncthreads();                                                         // everyone has read the old scale
     if (threadIdx.x == 0) *scale_at = scale;
+    const float inverse = 1.f / scale;
     int8_t* codes = (p.is_v ? j.v_codes : j.k_codes) + (p.page * j.heads + p.head) * (long long)(kPage * j.pitch);
-    if (p.is_v) {
-        // four tokens of a channel to a word of codes
-        for (int i = threadIdx.x; i < j.dim * (kPage / 4); i += kThreads) {
-            const int c = i / (kPage / 4), t = (i % (kPage / 4)) * 4;
-            if (t >= t1 || (t + 3 < t0 && ratio == 1.f)) continue;
-            unsigned* at = (unsigned*)(codes + c * kPage + t);
-            unsigned word = t < t0 || t + 3 >= t1 ? *at : 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int tt = t + e;
-                if (tt >= t1) continue;
-                int q = (int8_t)(word >> (8 * e));
-                if (tt >= t0) q = code_of(vals[(tt - t0) * pitch + c], scale);
-                else if (ratio != 1.f) q = (int)rintf((float)q * ratio);
-                word = (word & ~(0xffu << (8 * e))) | (unsigned)(q & 0xff) << (8 * e);
+    if (!p.is_v) {
+        if (ratio != 1.f)
+            for (int i = threadIdx.x; i < t0 * (j.dim / 4); i += kThreads) {
+                unsigned* at = (unsigned*)(codes + i / (j.dim / 4) * j.pitch + i % (j.dim / 4) * 4);
+                *at = smaller(*at, ratio);
             }
-            *at = word;
-        }
-    } else {
-        const int words = j.dim / 4;
-        for (int i = threadIdx.x + (ratio == 1.f ? t0 * words : 0); i < t1 * words; i += kThreads) {
-            const int t = i / words, c = (i % words) * 4;
-            unsigned* at = (unsigned*)(codes + t * j.pitch + c);
-            unsigned word = t < t0 ? *at : 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                int q = (int8_t)(word >> (8 * e));
-                if (t >= t0) q = code_of(vals[(t - t0) * pitch + c + e], scale);
-                else q = (int)rintf((float)q * ratio);
-                word = (word & ~(0xffu << (8 * e))) | (unsigned)(q & 0xff) << (8 * e);
+        for (int q = 0; q < kPasses; ++q)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int t = 4 * (set + q * sets) + i;
+                if (set < sets && t >= t0 && t < t1) {
+                    float f[VEC];
+                    unpack(v[q][i], f);
+                    int8_t* at = codes + t * j.pitch + c;
+                    if constexpr (VEC >= 4) {
+                        Pack<unsigned, VEC / 4> w;
+#pragma unroll
+                        for (int k = 0; k < VEC / 4; ++k) {
+                            const float g[4] = {f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]};
+                            w.v[k] = codes_of(g, scale, inverse);
+                        }
+                        *(Pack<unsigned, VEC / 4>*)at = w;
+                    } else {
+                        const float g[4] = {f[0], 0.f, 0.f, 0.f};
+                        *at = (int8_t)codes_of(g, scale, inverse);
+                    }
+                }
             }
-            *at = word;
+        return;
+    }
+    if (set < sets)
+#pragma unroll
+        for (int q = 0; q < kPasses; ++q) {
+            const int t = 4 * (set + q * sets);
+            if (t < kPage && t + 4 > t0 && t < t1) {
+                float f[4][VEC];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (t + i >= t0 && t + i < t1) {
+                        unpack(v[q][i], f[i]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) f[i][e] = 0.f;
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float g[4] = {f[0][e], f[1][e], f[2][e], f[3][e]};
+                    turned[(c + e) * kRow + t / 4] = codes_of(g, scale, inverse);
+                }
+            }
         }
+    __syncthreads();
+    for (int i = threadIdx.x; i < j.dim * (kPage / 16); i += kThreads) {
+        const int ch = i / (kPage / 16), t = i % (kPage / 16) * 16;
+        if (t >= t1 || (t + 16 <= t0 && ratio == 1.f)) continue;
+        Pack<unsigned, 4>* at = (Pack<unsigned, 4>*)(codes + ch * kPage + t);
+        Pack<unsigned, 4> w = *(const Pack<unsigned, 4>*)(turned + ch * kRow + t / 4);
+        if (t < t0 || t + 16 > t1) {                                         // codes that stay
+            const Pack<unsigned, 4> was = *at;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int a = t + 4 * k;                                     // bytes a .. a + 3, of which t0 <= byte < t1 are new
+                unsigned fresh = 0xffffffffu;
+                if (a < t0) fresh = a + 4 <= t0 ? 0u : fresh << (8 * (t0 - a));
+                if (a + 4 > t1) fresh &= a >= t1 ? 0u : 0xffffffffu >> (8 * (a + 4 - t1));
+                const unsigned kept = ratio != 1.f && a < t0 ? smaller(was.v[k], ratio) : was.v[k];
+                w.v[k] = (w.v[k] & fresh) | (kept & ~fresh);
+            }
+        }
+        *at = w;
     }
 }
 
-// Values of a page and head back, through LDS where the tokens lie side by side.
-template <typename T, int VEC>
+// Values of a page and head back: a thread has eight channels of four tokens.
+template <typename T, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void k_cache_read(CacheJob j) {
-    extern __shared__ unsigned words[];                                      // [dim][kPage / 4 + 1]
+    extern __shared__ __align__(16) unsigned turned[];                       // values: [dim][kPage / 4 + 4]
+    constexpr int kRow = kPage / 4 + 4;
     PageOf p;
     if (!p.find(j)) return;
     const CacheMap& m = p.is_v ? j.v : j.k;
     const int base = p.slot * kPage;
     const int t0 = max(p.first - base, 0), t1 = min(p.count - (base - p.first), kPage);
-    const long long row0 = (long long)p.row + (base - p.first);
-    T* y = (T*)m.y + p.head * m.y_head;
-    const long long at = p.page < 0 ? 0 : p.page * j.heads + p.head;
-    const float scale = p.page < 0 ? 0.f : (p.is_v ? j.v_scale : j.k_scale)[at];
+    T* y = (T*)m.y + p.head * m.y_head + ((long long)p.row + (base - p.first)) * m.y_token;
+    const bool there = p.page >= 0;
+    const long long at = there ? p.page * j.heads + p.head : 0;
+    const float scale = there ? (p.is_v ? j.v_scale : j.k_scale)[at] : 0.f;
     const int8_t* codes = (p.is_v ? j.v_codes : j.k_codes) + at * (kPage * j.pitch);
-    constexpr int kRow = kPage / 4 + 1;
-    if (p.is_v && p.page >= 0) {
-        for (int i = threadIdx.x; i < j.dim * (kPage / 4); i += kThreads) {
-            const int c = i / (kPage / 4), w = i % (kPage / 4);
-            words[c * kRow + w] = *(const unsigned*)(codes + c * kPage + w * 4);
-        }
+    if (p.is_v && there) {
+        for (int i = threadIdx.x; i < j.dim * (kPage / 16); i += kThreads)
+            *(Pack<unsigned, 4>*)(turned + i / (kPage / 16) * kRow + i % (kPage / 16) * 4) = *(const Pack<unsigned, 4>*)(codes + i * 16);
         __syncthreads();
     }
-    const int vecs = j.dim / VEC;
-    for (int i = threadIdx.x; i < (t1 - t0) * vecs; i += kThreads) {
-        const int t = t0 + i / vecs, c = (i % vecs) * VEC;
-        float f[VEC];
+    const int vecs = j.dim / 8, sets = kThreads / vecs, set = threadIdx.x / vecs, c = (threadIdx.x - set * vecs) * 8;
+    if (set >= sets) return;
+    for (int t = 4 * set; t < t1; t += 4 * sets) {
+        if (t + 4 <= t0) continue;
+        unsigned w[8];                                                       // values: word e has channel c + e of the four tokens; keys: words 2 i, 2 i + 1 token i
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            int q = 0;
-            if (p.page >= 0) q = p.is_v ? (int8_t)(words[(c + e) * kRow + t / 4] >> (8 * (t & 3))) : codes[t * j.pitch + c + e];
-            f[e] = p.page >= 0 ? (float)q * scale : 0.f;
+        for (int e = 0; e < 8; ++e) w[e] = there ? p.is_v ? turned[(c + e) * kRow + t / 4] : *(const unsigned*)(codes + (t + e / 2) * j.pitch + c + e % 2 * 4) : 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (t + i < t0 || t + i >= t1) continue;
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int q = p.is_v ? (int8_t)(w[e] >> (8 * i)) : (int8_t)(w[2 * i + e / 4] >> (8 * (e % 4)));
+                f[e] = there ? (float)q * scale : 0.f;
+            }
+            T* to = y + (t + i) * m.y_token + c;
+            if constexpr (WHOLE) {
+                constexpr int N = 16 / sizeof(T);
+#pragma unroll
+                for (int k = 0; k < 8 / N; ++k) {
+                    float g[N];
+#pragma unroll
+                    for (int e = 0; e < N; ++e) g[e] = f[N * k + e];
+                    *(Pack<T, N>*)(to + N * k) = pack<T, N>(g);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) to[e] = (T)f[e];
+            }
         }
-        *(Pack<T, VEC>*)(y + (row0 + t) * m.y_token + c) = pack<T, VEC>(f);
     }
 }
 
 template <typename T, int VEC>
 hipError_t launch(const CacheJob& j, bool store, hipStream_t st) {
     const dim3 grid((unsigned)(j.n_seq * j.slots), (unsigned)(2 * j.heads));
-    if (store) k_cache_store<T, VEC><<<grid, kThreads, (size_t)min(kPage, j.max_new) * (j.dim + 1) * 4, st>>>(j);
-    else k_cache_read<T, VEC><<<grid, kThreads, (size_t)j.dim * (kPage / 4 + 1) * 4, st>>>(j);
+    const size_t lds = (size_t)j.dim * (kPage / 4 + 4) * 4;
+    if (store) k_cache_store<T, VEC><<<grid, kThreads, lds, st>>>(j);
+    else k_cache_read<T, (VEC > 1)><<<grid, kThreads, lds, st>>>(j);
     return hipGetLastError();
 }
 

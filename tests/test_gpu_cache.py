@@ -97,6 +97,16 @@ def test_zeros_small_values_and_values_that_are_not_finite():
         same(c, rk, rv, table, [20])
 
 
+@pytest.mark.parametrize("amp", [1e-37, 3e-38, 1e-39, 1e-42])
+def test_scales_without_a_finite_reciprocal(amp):
+    """Values so small that their scale is subnormal: codes as the quotients say, to the bit."""
+    g = torch.Generator().manual_seed(3)
+    c, rk, rv = make(2, 2, 40)
+    for counts, held in (([70], [0]), ([5], [70])):
+        put(c, rk, rv, [[1, 0]], counts, held, torch.float32, g, amp)
+        same(c, rk, rv, [[1, 0]], [held[0] + counts[0]])
+
+
 def test_a_page_that_grows_at_every_token_stays_within_its_bound():
     """64 tokens, each a little larger than the last: half a code for the last rounding and half of 0.8 + 0.64 + .. = 4 for the earlier ones."""
     c, rk, rv = make(1, 1, 32)
