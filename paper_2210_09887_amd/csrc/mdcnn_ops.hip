@@ -69,7 +69,8 @@ int plan_norm(const mdcnn_group_norm_desc& d, bool backward, int vec, NormJob& j
     j.gamma = d.gamma_dev; j.beta = d.beta_dev;
     const int unit = std::lcm(j.cpg, vec);         // a slice holds whole groups and whole vectors
     const int esize = (int)storage_bytes(d.dtype), images = std::max(d.N, 1);
-    // Held in registers: slices of 64 bytes of channels (a memory segment) at least, threads so that the LDS takes 32 KiB.
+    // Held in registers: slices of 64 bytes of channels (a memory segment) at least, threads so that the LDS takes 32 KiB.  Held / in chunks, forward and
+    // backward: 12 x 9 x 256 16 / 28 us, 24 x 18 x 128 19 / 30, 16 maps of 16 x 16 x 512 25 / 33, of 32 x 32 x 256 (forward only) 14 / 18.
     {
         const int most = std::min(1024, 4096 / vec), deep = backward ? 4 : 8;
         int slice = unit * std::max(1, (64 / esize + unit - 1) / unit);
@@ -86,7 +87,8 @@ int plan_norm(const mdcnn_group_norm_desc& d, bool backward, int vec, NormJob& j
         }
     }
     // In chunks: up to 128 vectors beside one another, so that few of 256 threads are left over; 32 vectors to a thread, fewer
-    // (down to 4) where that leaves less than four blocks to a compute unit.
+    // (down to 4) where that leaves less than four blocks to a compute unit.  (Forward and backward of 16 bf16 maps of 128 x 128 x 256: 16 vectors 234 us,
+    // 32 223, 64 238.)
     j.slice = std::min(j.C, unit * std::max(1, 128 * vec / unit));
     j.slices = (j.C + j.slice - 1) / j.slice;
     j.lanes = std::min(j.slice / vec, kNormThreads);
@@ -229,8 +231,9 @@ mdcnn_status check_attend(const mdcnn_cache_desc* c, const mdcnn_attend_desc* a,
     return MDCNN_OK;
 }
 
-// Rows to a block and pages to a split.  Up to 32 rows go by sixteen, one or two blocks that each read the cache; more by 128, whose codes are
-// read once and made halves once.
+// Rows to a block and pages to a split.  Up to 64 rows go by sixteen, blocks that each read the cache (from the second on mostly out of the L2); more by 128,
+// whose codes are read once and made halves once.  16 sequences of 8192 tokens, 8 heads of 128 channels, by sixteen / by 128: 16 rows 50 / 104 us,
+// 48 rows 103 / 135, 64 rows 122 / 139, 128 rows 233 / 193; 64 of 1024 tokens, 64 channels: 64 rows 43 / 48, 128 rows 79 / 66.
 // Runs of 12 to 32 pages by sixteen rows: shorter ones are mostly what a block does once (its queries, its sums: two sequences of 150001 tokens, 2 heads,
 // 60 us with 4 pages, 45 with 8, 37 with 24), longer ones leave the last blocks of ragged sequences alone on the GPU; in between just under the 512 blocks that
 // the GPU holds.  By 128 rows about 2048 blocks, whose weights and sums for the splits are a tenth of a run of 24 pages.
@@ -241,7 +244,7 @@ mdcnn_status plan_attend(const mdcnn_cache_desc& c, const mdcnn_attend_desc& a, 
     j.causal = a.causal; j.window = a.window; j.scale = a.scale;
     const long long rows = (long long)j.max_new * j.group;
     if (rows > 0x7fffff00ll || rows * c.n_seq * c.heads > 0x7fffffffll) return fail(MDCNN_ERR_SIZE, "cache_attend: too many rows");
-    j.tile_rows = rows <= 32 || !attend_tiles_fit(dtype, j.pitch) ? kAttendRows : kAttendTile;
+    j.tile_rows = rows <= 64 || !attend_tiles_fit(dtype, j.pitch) ? kAttendRows : kAttendTile;
     j.tiles = (int)((rows + j.tile_rows - 1) / j.tile_rows);
     const long long columns = (long long)j.tiles * c.n_seq * c.heads;
     long long most = std::min<long long>((a.max_len + (long long)MDCNN_PAGE_TOKENS - 1) / MDCNN_PAGE_TOKENS, c.max_pages);
@@ -348,7 +351,8 @@ mdcnn_status mdcnn_rotary(const mdcnn_heads* maps, int n_maps, int tokens, int d
     j.units = j.turned_units + (in_place ? 0 : (dim - turned) / vec);
     j.tokens_per_block = 256 / j.units;
     j.inverse = inverse; j.magnitude = magnitude;
-    // A thread goes through up to 16 heads with the same sines; fewer where that leaves less than eight blocks to a compute unit.
+    // A thread goes through up to 16 heads with the same sines; fewer where that leaves less than eight blocks to a compute unit.  (40 bf16 heads of 128
+    // channels: 32768 tokens 130 us, one head to a thread 147; 48 tokens 3.6 us, 16 heads to a thread 9.1.)
     const int heads = j.maps[0].heads + j.maps[1].heads;
     const long long blocks = (tokens + j.tokens_per_block - 1) / j.tokens_per_block;
     j.group = std::min(heads, 16);
