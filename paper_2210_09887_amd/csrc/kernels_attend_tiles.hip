@@ -36,10 +36,10 @@ struct Stage {
 // LDS is waited for, loads from memory are not.
 __device__ __forceinline__ void page_over() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// Waves to a SIMD, as queries, sums, products and weights leave room for them.  More of them help: one wave issues a vector instruction every five
+// More waves to a SIMD help: one wave issues a vector instruction every five
 // cycles, two or three together one every three.  (64 channels of 16 bits: two waves 1744 us for 4 x 4096 queries of 32 heads over 8192 tokens, three 1602.)
 template <typename T, int DP, bool MASK>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (DP <= 64 ? 3 : DP <= 128 ? 2 : 1) : (DP == 32 ? 3 : DP <= 96 ? 2 : 1)) void k_attend_tiles(AttendJob j) {
+__global__ __launch_bounds__(kThreads, attend_tile_blocks(sizeof(T), DP)) void k_attend_tiles(AttendJob j) {
     constexpr bool kTwo = sizeof(T) == 4;
     constexpr int NS = DP / 16, ND = DP / 32, NL = DP / 32;               // steps of channels, tiles of channels, 16-byte loads of a thread
     constexpr int kHeld = DP > 192 ? 9 : NS;                              // steps of the queries in registers; the others lie in LDS behind the two stages

@@ -236,7 +236,9 @@ mdcnn_status check_attend(const mdcnn_cache_desc* c, const mdcnn_attend_desc* a,
 // 48 rows 103 / 135, 64 rows 122 / 139, 128 rows 233 / 193; 64 of 1024 tokens, 64 channels: 64 rows 43 / 48, 128 rows 79 / 66.
 // Runs of 12 to 32 pages by sixteen rows: shorter ones are mostly what a block does once (its queries, its sums: two sequences of 150001 tokens, 2 heads,
 // 60 us with 4 pages, 45 with 8, 37 with 24), longer ones leave the last blocks of ragged sequences alone on the GPU; in between just under the 512 blocks that
-// the GPU holds.  By 128 rows about 2048 blocks, whose weights and sums for the splits are a tenth of a run of 24 pages.
+// the GPU holds.  By 128 rows as many runs as the GPU holds blocks, but none shorter than 8 pages: a run leaves its sums in 32 bits, and one that begins when others
+// end leaves the GPU half empty (against about 2048 blocks: prompt of 2000 tokens, 32 heads of 128 channels over 8, 90 and 140 us; two prompts of 1300
+// and 700 behind 4000 and 2000, 64 channels, 85 and 94; 1000 rows over 8192 tokens, 8 heads of 128 channels, 105 and 110).
 mdcnn_status plan_attend(const mdcnn_cache_desc& c, const mdcnn_attend_desc& a, int q_heads, int dtype, AttendJob& j, size_t* bytes) {
     j.pages = c.pages; j.heads = c.heads; j.group = q_heads / c.heads; j.dim = c.dim; j.pitch = mdcnn_cache_pitch(c.dim);
     j.n_seq = c.n_seq; j.max_pages = c.pages ? c.max_pages : 0;
@@ -247,14 +249,17 @@ mdcnn_status plan_attend(const mdcnn_cache_desc& c, const mdcnn_attend_desc& a, 
     j.tile_rows = rows <= 64 || !attend_tiles_fit(dtype, j.pitch) ? kAttendRows : kAttendTile;
     j.tiles = (int)((rows + j.tile_rows - 1) / j.tile_rows);
     const long long columns = (long long)j.tiles * c.n_seq * c.heads;
+    const long long live = std::min(columns, ((long long)j.tokens * j.group / j.tile_rows + c.n_seq) * c.heads);        // (no more of them have rows)
     long long most = std::min<long long>((a.max_len + (long long)MDCNN_PAGE_TOKENS - 1) / MDCNN_PAGE_TOKENS, c.max_pages);
     if (a.window) most = std::min<long long>(most, (a.window + (long long)j.max_new + 2 * MDCNN_PAGE_TOKENS - 2) / MDCNN_PAGE_TOKENS);
     most = std::max(most, 1ll);
-    auto per = [&](long long blocks) { return (int)((most * columns + blocks - 1) / blocks); };
-    j.run = j.tile_rows == kAttendRows ? std::min(32, std::max(12, per(480))) : (int)std::min<long long>(most, std::max(8, per(2048)));
-    j.splits = (int)((most + j.run - 1) / j.run);
-    j.run = (int)((most + j.splits - 1) / j.splits);                       // all alike
-    if (columns >= (j.tile_rows == kAttendRows ? 2048 : 1024)) { j.splits = 1; j.run = 1 << 30; }
+    if (j.tile_rows == kAttendRows) {
+        const long long run = std::min(32ll, std::max(12ll, (most * live + 479) / 480));
+        j.splits = live >= 2048 ? 1 : (int)((most + run - 1) / run);
+    } else {
+        j.splits = (int)std::max(1ll, std::min((most + 7) / 8, 256ll * attend_tile_blocks((int)storage_bytes(dtype), j.pitch) / std::max(1ll, live)));
+    }
+    j.run = j.splits == 1 ? 1 << 30 : (int)((most + j.splits - 1) / j.splits);          // all alike
     if (columns * j.splits > 0x7fffffffll) return fail(MDCNN_ERR_SIZE, "cache_attend: too large");
     *bytes = j.splits > 1 ? (size_t)columns * j.splits * j.tile_rows * (8 + 4 * (size_t)j.pitch) + 256 : 0;
     return MDCNN_OK;

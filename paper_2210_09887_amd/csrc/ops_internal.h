@@ -107,5 +107,7 @@ bool attend_tiles_fit(int dtype, int pitch);             // whether launch_atten
 hipError_t launch_attend_tiles(const AttendJob& j, int dtype, hipStream_t st);
 hipError_t launch_attend_join(const AttendJob& j, int dtype, hipStream_t st);     // nothing if there is one split
 constexpr int kAttendRows = 16, kAttendTile = 128;       // rows of a block of the two
+// Blocks of 128 rows on a compute unit (waves on a SIMD), as queries, sums, products and weights leave room for them in the registers.
+constexpr int attend_tile_blocks(int value_bytes, int pitch) { return value_bytes == 2 ? (pitch <= 64 ? 3 : pitch <= 128 ? 2 : 1) : pitch == 32 ? 3 : pitch <= 96 ? 2 : 1; }
 
 }  // namespace mdcnn
