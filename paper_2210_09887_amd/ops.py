@@ -13,6 +13,7 @@ from __future__ import annotations
 import functools
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -137,17 +138,18 @@ class _GroupNormAct(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, gamma, beta, mean, rstd = ctx.saved_tensors
         groups, act = ctx.how
         if not _beside(dy.shape, dy.stride()):
             dy = dy.contiguous()
         dx, dgamma, dbeta = group_norm_backward(x, dy, mean, rstd, groups, gamma, beta, act)
-        return dx, None, None if gamma is None else dgamma, None if beta is None else dbeta, None, None
+        return dx, None, None if gamma is None else dgamma.view_as(gamma), None if beta is None else dbeta.view_as(beta), None, None
 
 
 def group_norm_act(x, groups, gamma=None, beta=None, eps=1e-5, act="none"):
-    """y of group_norm for autograd: gradients of x, gamma and beta."""
+    """y of group_norm for autograd: gradients of x, gamma and beta (which may have any shape of C values); not differentiable twice."""
     return _GroupNormAct.apply(x, groups, gamma, beta, eps, act)
 
 
@@ -205,6 +207,7 @@ class _Rotary(torch.autograd.Function):
         return tuple(rotary(maps, positions, steps, axes, interleaved, magnitude))
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, *grads):
         positions, steps = ctx.saved_tensors
         axes, interleaved, magnitude = ctx.how
@@ -213,7 +216,7 @@ class _Rotary(torch.autograd.Function):
 
 
 def rotary_turn(maps, positions, steps, axes=1, interleaved=False, magnitude=1.0):
-    """`rotary` for autograd: gradients of the maps."""
+    """`rotary` for autograd: gradients of the maps; not differentiable twice."""
     return list(_Rotary.apply(positions, steps, axes, interleaved, magnitude, *maps))
 
 

@@ -196,6 +196,21 @@ def test_autograd():
     y.sum().backward()                                   # a gradient of stride 0
 
 
+def test_scales_of_another_shape_and_no_second_gradient():
+    from paper_2210_09887_amd import ops
+    x, gamma, beta, dy = (t.cuda() for t in inputs(2, 5, 6, 24, torch.float32, 13))
+    a = [t.clone().requires_grad_() for t in (x, gamma, beta)]
+    ops.group_norm_act(a[0], 3, a[1], a[2], act="silu").backward(dy)
+    b = [x.clone().requires_grad_(), gamma.view(1, 1, 1, 24).clone().requires_grad_(), beta.view(24, 1).clone().requires_grad_()]
+    y = ops.group_norm_act(b[0], 3, b[1], b[2], act="silu")
+    y.backward(dy, retain_graph=True)
+    assert b[1].grad.shape == (1, 1, 1, 24) and b[2].grad.shape == (24, 1)
+    assert all(torch.equal(p.grad.flatten(), q.grad.flatten()) for p, q in zip(a, b))
+    g, = torch.autograd.grad(y, b[0], dy.clone().requires_grad_(), create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
+
+
 def test_no_images():
     from paper_2210_09887_amd import ops
     x = torch.empty((0, 4, 4, 8), device="cuda")

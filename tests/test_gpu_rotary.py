@@ -127,6 +127,19 @@ def test_gradient_is_the_transposed_turn():
     assert abs(a - b) < 2.0 ** -18 * float(q.norm() * dq.norm())
 
 
+def test_a_map_that_the_loss_leaves_out_and_no_second_gradient():
+    from paper_2210_09887_amd import ops
+    q, k = (torch.randn((7, 3, 16), device="cuda", requires_grad=True) for _ in range(2))
+    pos, steps = torch.arange(7, dtype=torch.int32, device="cuda"), ops.rotary_steps(16)
+    out = ops.rotary_turn((q, k), pos, steps)
+    d = torch.randn_like(out[0])
+    out[0].backward(d, retain_graph=True)
+    assert torch.equal(q.grad, ops.rotary((d,), pos, steps, inverse=True)[0]) and not bool(k.grad.any())
+    g, = torch.autograd.grad(out[0], q, d.clone().requires_grad_(), create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
+
+
 def test_no_tokens_and_refusals():
     from paper_2210_09887_amd import ops
     steps, pos = ops.rotary_steps(8), torch.zeros(3, dtype=torch.int32, device="cuda")
