@@ -8,9 +8,11 @@
 //
 // Codes become halves without a conversion: a byte c + 128 in the low byte of 0x6400 is the half 1152 + c, minus 1152 is c,
 // exactly.  The scale of a page's keys is multiplied into the logits.  That of its values goes into the exponent,
-//   w = 2^(x + log2 vs - T),  T the row's largest x + log2 vs so far,
-// so that w is a half of full precision next to what counts most in this row, whatever the sizes of scales and values: sum w code / sum (w / vs)
-// is the result, 2^T sum (w / vs) the sum of the exponentials.  T is moved by pages that have values: those that are all zeros (vs below 2^-100) or not
+//   w = 2^(x + log2 vs - T + kRoom),  T the row's largest x + log2 vs so far,
+// so that w is a half next to what counts most in this row, whatever the sizes of scales and values: sum w code / sum (w / vs) is the result,
+// 2^(T - kRoom) sum (w / vs) the sum of the exponentials.  Weights near 2^kRoom at the top leave the halves' range to those below: one has all its bits
+// down to 2^-24 of the largest, and a step of 2^-34 of it from there (a first token 14 above 4096 others: with the largest at 1 the others' part of the result
+// was off by 1 %).  T is moved by pages that have values: those that are all zeros (vs below 2^-100) or not
 // numbers count in the second sum only, with the scale of the page before.  (Scales of one sequence and head may lie 2^100 apart.)
 #pragma once
 
@@ -74,17 +76,21 @@ struct Run {
     }
 };
 
+// Where weights lie: the largest that T knows at 2^kRoom.  32 of them in a lane (a page of the tiles) add up to 2^15 then, below kMuch.
+constexpr float kRoom = 10.f, kUnroom = 1.f / 1024;
+
 // The scale of a page's values in the exponent.  Its logarithm is rounded to 32 bits, which takes up to 2^-21 of the values; the inverse is that of the
 // rounded one, so that the sum of the exponentials does not notice.
+// The inverse takes kRoom out of the sum again.
 struct ValueScale {
-    float log = 0.f, inverse = 1.f;
+    float log = 0.f, inverse = kUnroom;
     bool none = false, bad = false;                        // weights do not count in the sum of values; not a number
     __device__ __forceinline__ void next(float vs) {
         bad = vs != vs;
         none = vs < 7.8886090522101181e-31f;               // 2^-100; any scale does then: that of the page before
         if (!none && !bad) {
             log = __builtin_amdgcn_logf(vs);
-            inverse = exp2_fast(-log);
+            inverse = exp2_fast(-log) * kUnroom;
         }
     }
 };
@@ -95,8 +101,8 @@ __device__ __forceinline__ float factor_of(float logit, float ks) {
     return by < 1e-30f ? 1e-30f : by;
 }
 // T of a row is moved - and what has been summed faded - only where the weights of a lane add up to more than this (they have to be
-// halves, or finite where no values follow): weights are made before anyone looks for a maximum, and on nearly all pages no one does.
-constexpr float kMuch = 16384.f, kMuchNoValues = 18446744073709551616.f;
+// halves, of which the largest is 65504, or finite where no values follow): weights are made before anyone looks for a maximum, and on nearly all pages no one does.
+constexpr float kMuch = 65504.f, kMuchNoValues = 18446744073709551616.f;
 
 // T of a row after a page whose largest x + log2 vs is `most` (minus infinity: the row sees none of it), and what the sums fade by.  The first page with
 // values sets it, whatever pages without values left (their sum is kept: no further down than that stays finite).

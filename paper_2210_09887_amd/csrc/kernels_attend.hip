@@ -165,7 +165,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
             float add;
             half8 ph[2], pl[kTwo ? 2 : 1];
             auto weigh = [&]() {
-                const float base = val.log - (top == -INFINITY ? 0.f : top);
+                const float base = val.log - (top == -INFINITY ? 0.f : top) + kRoom;
                 float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int t = 0; t < 16; ++t) {
@@ -245,6 +245,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
         float x = 0.f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) x += weight[w] * s_out[w][m][c];
+        x *= kUnroom;
         if (!whole) j.part_out[(slot * 16 + m) * DP + c] = x;
         else if (c < j.dim) y[c] = (T)(x * inv);
     }

@@ -222,7 +222,7 @@ __global__ __launch_bounds__(kThreads, attend_tile_blocks(sizeof(T), DP)) void k
                 float add;
                 half8 ph[4], pl[kTwo ? 4 : 1];
                 auto weigh = [&]() {
-                    const float base = val.log - (top == -INFINITY ? 0.f : top);
+                    const float base = val.log - (top == -INFINITY ? 0.f : top) + kRoom;
                     float part[4];
 #pragma unroll
                     for (int t = 0; t < 32; ++t) {
@@ -310,10 +310,10 @@ __global__ __launch_bounds__(kThreads, attend_tile_blocks(sizeof(T), DP)) void k
         for (int q = 0; q < 4; ++q) {
             const int c = 32 * d + 8 * q + 4 * half;       // four channels beside one another
             if (!whole) {
-                *(float4v*)(j.part_out + slot * DP + c) = float4v{out[d][4 * q], out[d][4 * q + 1], out[d][4 * q + 2], out[d][4 * q + 3]};
+                *(float4v*)(j.part_out + slot * DP + c) = float4v{out[d][4 * q], out[d][4 * q + 1], out[d][4 * q + 2], out[d][4 * q + 3]} * kUnroom;
             } else if (c < j.dim) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) y[c + i] = (T)(out[d][4 * q + i] * inv);
+                for (int i = 0; i < 4; ++i) y[c + i] = (T)(out[d][4 * q + i] * kUnroom * inv);
             }
         }
     if (half == 0) {

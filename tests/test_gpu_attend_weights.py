@@ -1,0 +1,78 @@
+"""Attention where one token outweighs all others: the others' weights keep their bits, and with them what they add up to."""
+import math
+
+import pytest
+import torch
+
+from cache_ref import PAGE
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+EPS = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+HEADS, DIM = 8, 32
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def check_sink(tokens, queries, copies, gap, equal, sink_value, dtype, floor):
+    """The first of `tokens` tokens has a logit about `gap` above the others', which are all equal or a deviation of one apart; its values are zeros or like theirs.
+    `copies` sequences read the same pages with the same queries: with many of them a block goes over a whole sequence.
+
+    Bounds: a weight is a half (one of fp32 calls two) down to `floor` of the largest, whatever it is; logits of up to G from products and sums in 32 bits, 8 * 2^-24 G;
+    sums over the pages in 32 bits, four terms a page; the result rounded once."""
+    from paper_2210_09887_amd import ops
+    g = torch.Generator().manual_seed(tokens + queries)
+    pages, scale = -(-tokens // PAGE), DIM ** -0.5
+    k = torch.zeros((tokens, HEADS, DIM))
+    if not equal:
+        k[1:, :, 1:] = torch.randint(-20, 21, (tokens - 1, HEADS, DIM - 1), generator=g).float()
+    k[0, :, 0] = 100
+    v = torch.randint(20, 128, (tokens, HEADS, DIM), generator=g).float()
+    if sink_value == "zero":
+        v[0] = 0
+    q = torch.randn((queries, HEADS, DIM), generator=g) / (0.115 * math.sqrt(DIM - 1) * scale)
+    q[..., 0] = gap / scale
+    q = q.to(dtype)
+    c = ops.GpuCache.empty(pages, HEADS, DIM)
+    pad = pages * PAGE - tokens
+    lay = lambda t: torch.cat((t, torch.full((pad, HEADS, DIM), 77.0))).view(pages, PAGE, HEADS, DIM).permute(0, 2, 1, 3).to(torch.int8)  # noqa: E731
+    c.k.copy_(lay(k))
+    c.v.copy_(lay(v).transpose(2, 3))
+    c.k_scale.fill_(0.01)
+    c.v_scale.fill_(0.01)
+    table = ints([list(range(pages))] * copies)
+    starts = ints([queries * i for i in range(copies + 1)])
+    out, lse = c.attend(q.cuda().repeat(copies, 1, 1), table, starts, ints([tokens] * copies), queries, tokens)
+    held = float(torch.tensor(0.01))                     # the scales as they are held
+    score = torch.einsum("qhd,thd->hqt", q.double(), k.double()) * (held * float(torch.tensor(scale)))
+    top = score.amax(2, keepdim=True)
+    p = torch.exp(score - top)
+    total = p.sum(2, keepdim=True)
+    values = v.double().transpose(0, 1) * held
+    want = (p / total) @ values
+    if dtype == torch.float16 and float(want.abs().min()) < 2.0 ** -14:
+        return                                           # (halves do not resolve such results)
+    half = 2.0 ** -22 if dtype == torch.float32 else 2.0 ** -11
+    arithmetic = (8 * (abs(gap) + 6) + 4 * pages + 16) * 2.0 ** -24
+    bound = EPS[dtype] * want.abs() + ((half * p).clamp(min=floor) / total) @ values.abs() + arithmetic * ((p / total) @ values.abs())
+    got, logs = out.double().cpu().view(copies, queries, HEADS, DIM).transpose(1, 2), lse.double().cpu().view(copies, queries, HEADS).transpose(1, 2)
+    worst = float(((got - want).abs() / bound).max())
+    print(f"{dtype} {tokens} tokens, {queries} queries, gap {gap}, {'equal' if equal else 'uneven'}, sink {sink_value}: {worst:.3f} of the bound, "
+          f"relative {float((got[0] - want).norm() / want.norm()):.2e}", flush=True)
+    assert worst < 1
+    assert float((logs - (top + total.log())[..., 0]).abs().max()) < 2 * arithmetic * (1 + abs(gap) / 8)
+
+
+SHAPES = [(768, 1, 1), (4096, 1, 1), (4096, 130, 1), (2048, 130, 48), (16384, 1, 256)]     # .. the last two: one block goes over a whole sequence
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("tokens,queries,copies", SHAPES)
+@pytest.mark.parametrize("gap", [0.0, 10.0, 12.0, 14.0, 17.5, 20.0])
+def test_tokens_beside_one_that_outweighs_them(tokens, queries, copies, gap, dtype):
+    for equal in (True, False):
+        for sink_value in ("zero", "usual"):
+            check_sink(tokens, queries, copies, gap, equal, sink_value, dtype, 2.0 ** -35)
