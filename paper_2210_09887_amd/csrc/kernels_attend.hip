@@ -172,7 +172,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
                     const float w = exp2_fast(__builtin_fmaf(x[t], by, base));
                     part[t % 4] += w;
                     ph[t / 8][t % 8] = (_Float16)w;
-                    if constexpr (kTwo) pl[t / 8][t % 8] = (_Float16)(w - (float)ph[t / 8][t % 8]);
+                    if constexpr (kTwo) pl[t / 8][t % 8] = (_Float16)((w - (float)ph[t / 8][t % 8]) * kSecond);
                 }
                 add = (part[0] + part[1]) + (part[2] + part[3]);
             };
@@ -206,8 +206,8 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
                     out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, ph[0], out[v], 0, 0, 0);
                     out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, ph[1], out[v], 0, 0, 0);
                     if constexpr (kTwo) {
-                        out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, pl[0], out[v], 0, 0, 0);
-                        out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, pl[1], out[v], 0, 0, 0);
+                        out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a * kSecondBack, pl[0], out[v], 0, 0, 0);
+                        out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b * kSecondBack, pl[1], out[v], 0, 0, 0);
                     }
                     if (v % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }

@@ -229,7 +229,7 @@ __global__ __launch_bounds__(kThreads, attend_tile_blocks(sizeof(T), DP)) void k
                         const float w = exp2_fast(__builtin_fmaf(x[t / 16][t % 16], by, base));
                         part[t % 4] = t < 4 ? w : part[t % 4] + w;
                         ph[t / 8][t % 8] = (_Float16)w;
-                        if constexpr (kTwo) pl[t / 8][t % 8] = (_Float16)(w - (float)ph[t / 8][t % 8]);
+                        if constexpr (kTwo) pl[t / 8][t % 8] = (_Float16)((w - (float)ph[t / 8][t % 8]) * kSecond);
                         if (t % 8 == 7) __builtin_amdgcn_sched_barrier(0);           // eight at a time: registers are short
                     }
                     add = (part[0] + part[1]) + (part[2] + part[3]);
@@ -259,7 +259,7 @@ __global__ __launch_bounds__(kThreads, attend_tile_blocks(sizeof(T), DP)) void k
                         const int st = DP <= 128 ? i / ND : i % 4, d = DP <= 128 ? i % ND : i / 4;
                         const half8 v = *(const half8*)(now + S::value_at(32 * d + place, 4 * half + st));
                         out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph[st], out[d], 0, 0, 0);
-                        if constexpr (kTwo) out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl[st], out[d], 0, 0, 0);
+                        if constexpr (kTwo) out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v * kSecondBack, pl[st], out[d], 0, 0, 0);
                     }
                 };
                 auto spoil = [&]() __attribute__((always_inline)) {

@@ -76,3 +76,12 @@ def test_tokens_beside_one_that_outweighs_them(tokens, queries, copies, gap, dty
     for equal in (True, False):
         for sink_value in ("zero", "usual"):
             check_sink(tokens, queries, copies, gap, equal, sink_value, dtype, 2.0 ** -35)
+
+
+@pytest.mark.parametrize("tokens,queries,copies", SHAPES)
+@pytest.mark.parametrize("gap", [14.0, 17.5, 20.0, 24.0])
+def test_weights_of_fp32_calls_keep_two_halves_of_bits(tokens, queries, copies, gap):
+    """The second half holds 2^11 times what the first leaves: 22 bits down to 2^-24 of the largest weight and a step of 2^-45 of it from there."""
+    for equal in (True, False):
+        for sink_value in ("zero", "usual"):
+            check_sink(tokens, queries, copies, gap, equal, sink_value, torch.float32, 2.0 ** -46)
