@@ -669,7 +669,7 @@ typedef struct {              /* queries or keys: heads of `dim` channels, chann
     const void* x_dev;
     void* y_dev;              /* may be x_dev with the same strides                     */
     int heads;
-    long long x_token, x_head, y_token, y_head;   /* elements between tokens / heads    */
+    long long x_token, x_head, y_token, y_head;   /* elements between tokens / heads; of no account where there is one */
 } mdcnn_heads;
 /* One or two maps (queries and keys) of `tokens` tokens in one launch.  pos_dev: tokens x axes positions, any int32.
  * interleaved: 0 pairs (i, i + turned/2), 1 pairs (2 i, 2 i + 1).  inverse: 1 turns back (sin negated, still times magnitude):

@@ -162,11 +162,12 @@ mdcnn_status check_heads(const mdcnn_heads& m, const char* call, const char* wha
     if ((reads && !aligned(m.x_dev, e)) || (writes && !aligned(m.y_dev, e))) return fail(MDCNN_ERR_ALIGN, "%s: %s is misaligned", call, what);
     if (reads && (m.x_token < 0 || m.x_head < 0 || m.x_token > top || m.x_head > top)) return fail(MDCNN_ERR_SHAPE, "%s: strides of %s out of range", call, what);
     if (writes) {
-        // heads within tokens or tokens within heads: either way none may reach into the next
-        const bool within = m.heads == 1 || m.y_head >= dim;
-        if (m.y_token < dim || !within || m.y_token > top || m.y_head > top) return fail(MDCNN_ERR_SHAPE, "%s: heads of %s overlap", call, what);
-        if (m.heads > 1 && m.y_token >= m.y_head && m.y_token < (m.heads - 1) * m.y_head + dim) return fail(MDCNN_ERR_SHAPE, "%s: tokens of %s overlap", call, what);
-        if (m.heads > 1 && m.y_token < m.y_head && m.y_head < (tokens - 1) * m.y_token + dim) return fail(MDCNN_ERR_SHAPE, "%s: heads of %s overlap", call, what);
+        // heads within tokens or tokens within heads: either way none may reach into the next; where there is one of them its stride counts for nothing
+        const bool several = m.heads > 1, more = tokens > 1;
+        if (m.y_token > top || m.y_head > top) return fail(MDCNN_ERR_SHAPE, "%s: strides of %s out of range", call, what);
+        if ((more && m.y_token < dim) || (several && m.y_head < dim)) return fail(MDCNN_ERR_SHAPE, "%s: heads of %s overlap", call, what);
+        if (several && more && m.y_token >= m.y_head && m.y_token < (m.heads - 1) * m.y_head + dim) return fail(MDCNN_ERR_SHAPE, "%s: tokens of %s overlap", call, what);
+        if (several && more && m.y_token < m.y_head && m.y_head < (tokens - 1) * m.y_token + dim) return fail(MDCNN_ERR_SHAPE, "%s: heads of %s overlap", call, what);
     }
     return MDCNN_OK;
 }
@@ -204,7 +205,7 @@ mdcnn_status run_cache(const mdcnn_cache_desc* c, const mdcnn_heads* k, const md
         if (st) return st;
         const void* at = store ? m->x_dev : m->y_dev;
         const long long token = store ? m->x_token : m->y_token, head = store ? m->x_head : m->y_head;
-        if (!aligned(at, 16) || token % vec || (m->heads > 1 && head % vec)) vec = 1;
+        if (!aligned(at, 16) || (tokens > 1 && token % vec) || (m->heads > 1 && head % vec)) vec = 1;
         (m == k ? j.k : j.v) = CacheMap{m->x_dev, m->y_dev, m->x_token, m->x_head, m->y_token, m->y_head};
     }
     j.k_codes = c->k_dev; j.v_codes = c->v_dev; j.k_scale = c->k_scale_dev; j.v_scale = c->v_scale_dev;
@@ -344,7 +345,7 @@ mdcnn_status mdcnn_rotary(const mdcnn_heads* maps, int n_maps, int tokens, int d
         bool ok = (interleaved ? turned : turned / 2) % v == 0 && (dim - turned) % v == 0;
         for (int i = 0; i < n_maps; ++i) {
             const RotaryMap& m = j.maps[i];
-            ok = ok && aligned(m.x, bytes) && aligned(m.y, bytes) && m.x_token % v == 0 && m.y_token % v == 0 && (m.heads == 1 || (m.x_head % v == 0 && m.y_head % v == 0));
+            ok = ok && aligned(m.x, bytes) && aligned(m.y, bytes) && (tokens == 1 || (m.x_token % v == 0 && m.y_token % v == 0)) && (m.heads == 1 || (m.x_head % v == 0 && m.y_head % v == 0));
         }
         if (ok) { vec = v; break; }
     }
@@ -411,7 +412,7 @@ mdcnn_status mdcnn_cache_attend(const mdcnn_cache_desc* c, const mdcnn_attend_de
     j.starts = a->starts_dev; j.lengths = a->lengths_dev; j.mask = a->mask_dev; j.mask_row = a->mask_row;
     j.mask_whole = aligned(a->mask_dev, 16) && (c->n_seq == 1 || a->mask_row % 16 == 0);
     const long long per = 16 / (long long)storage_bytes(dtype);
-    j.q_whole = aligned(q->x_dev, 16) && q->x_token % per == 0 && (q->heads == 1 || q->x_head % per == 0);
+    j.q_whole = aligned(q->x_dev, 16) && (a->tokens == 1 || q->x_token % per == 0) && (q->heads == 1 || q->x_head % per == 0);
     j.part_out = (float*)work_dev;
     j.part_top = (float2*)((char*)work_dev + (size_t)j.n_seq * j.heads * j.tiles * j.splits * j.tile_rows * j.pitch * 4);
     const auto first = j.tile_rows == kAttendRows ? launch_attend_rows : launch_attend_tiles;

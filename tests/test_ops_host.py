@@ -151,3 +151,14 @@ def test_attend_workspace():
     assert B.mdcnn_cache_attend_bytes(c, a, 8, 1) > 0 and B.mdcnn_cache_attend_bytes(c, attending(max_len=100), 8, 1) == 0
     refused(2, B.mdcnn_cache_attend_bytes, c, a, 6, 1)
     refused(3, B.mdcnn_cache_attend_bytes, c, a, 8, 7)
+
+
+def test_one_token_has_no_token_stride():
+    """[heads, 1, dim] seen as [1, heads, dim]: the checks get past the heads to what is refused behind them."""
+    for token in (32, 0, 1, 31, 95, 1 << 40):
+        one = heads(x_token=max(0, token), y_token=token)
+        refused(1, B.mdcnn_rotary, [one], 1, 32, 0, None, 1, FAKE, 32)
+        refused(4, B.mdcnn_cache_attend, cache(), attending(tokens=1, max_new=1), one, 1, FAKE + 2, FAKE, 1 << 40)
+        refused(4, B.mdcnn_cache_read, cache(), one, heads(y_dev=FAKE + 1), 1, FAKE, FAKE, 1, 1)
+    refused(2, B.mdcnn_rotary, [heads(y_head=31)], 1, 32, 0, None, 1, FAKE, 32)          # heads that overlap still do
+    refused(2, B.mdcnn_rotary, [heads(y_token=32)], 2, 32, 0, None, 1, FAKE, 32)         # and so do tokens, where there are two
