@@ -178,7 +178,9 @@ mdcnn_status check_cache(const mdcnn_cache_desc* c, const char* call) {
     if (!mdcnn_cache_pitch(c->dim)) return fail(MDCNN_ERR_SHAPE, "%s: %d channels to a head (8 to 256, a multiple of 8)", call, c->dim);
     if (c->heads < 1 || c->heads > 32767) return fail(MDCNN_ERR_SHAPE, "%s: %d heads", call, c->heads);
     if (c->pages < 0 || c->n_seq < 0 || c->max_pages < 0 || c->max_pages > (1 << 24)) return fail(MDCNN_ERR_SIZE, "%s: pages, sequences or table out of range", call);
-    if (c->n_seq && (!c->k_dev || !c->v_dev || !c->k_scale_dev || !c->v_scale_dev || !c->table_dev)) return fail(MDCNN_ERR_NULL, "%s: NULL pointer in the cache", call);
+    // (an empty tensor has no memory: a table without entries, a pool without pages)
+    const bool table = c->n_seq && c->max_pages, pool = table && c->pages;
+    if ((table && !c->table_dev) || (pool && (!c->k_dev || !c->v_dev || !c->k_scale_dev || !c->v_scale_dev))) return fail(MDCNN_ERR_NULL, "%s: NULL pointer in the cache", call);
     if (!aligned(c->k_dev, 16) || !aligned(c->v_dev, 16) || !aligned(c->k_scale_dev, 4) || !aligned(c->v_scale_dev, 4) || !aligned(c->table_dev, 4))
         return fail(MDCNN_ERR_ALIGN, "%s: misaligned pointer in the cache", call);
     return MDCNN_OK;

@@ -162,3 +162,12 @@ def test_one_token_has_no_token_stride():
         refused(4, B.mdcnn_cache_read, cache(), one, heads(y_dev=FAKE + 1), 1, FAKE, FAKE, 1, 1)
     refused(2, B.mdcnn_rotary, [heads(y_head=31)], 1, 32, 0, None, 1, FAKE, 32)          # heads that overlap still do
     refused(2, B.mdcnn_rotary, [heads(y_token=32)], 2, 32, 0, None, 1, FAKE, 32)         # and so do tokens, where there are two
+
+
+@pytest.mark.parametrize("kw", [dict(max_pages=0, table_dev=None), dict(pages=0, k_dev=None, v_dev=None, k_scale_dev=None, v_scale_dev=None), dict(pages=0, max_pages=0, table_dev=None, k_dev=None)])
+def test_a_cache_without_pages_or_a_table_without_entries_needs_no_memory(kw):
+    """The checks get past the cache to what is refused behind it."""
+    assert B.mdcnn_cache_attend_bytes(cache(**kw), attending(), 8, 1) == 0
+    refused(4, B.mdcnn_cache_attend, cache(**kw), attending(), heads(heads=8, x_token=256, y_token=256), 1, FAKE + 2, None, 0)
+    for call in (B.mdcnn_cache_store, B.mdcnn_cache_read):
+        refused(1, call, cache(**kw), heads(), heads(), 3, None, FAKE, 3, 1)
