@@ -2,7 +2,8 @@
 keys and values in 8 bits and the attention that reads it.
 
 Argument marshalling only: shapes, strides and types are taken from the tensors, outputs and workspaces come from torch, the
-work is enqueued on the current stream of the tensors' device.  `group_norm_act` and `rotary_turn` are the same for autograd.
+work is enqueued on the current stream of the tensors' device.  `group_norm_act` and `rotary_turn` are the same for autograd; the other calls know no
+gradients and refuse tensors that require one while autograd records.
 
 A call on a small map is as long as its way through the host, so what follows from shapes, strides and types alone - the checks, the description
 for the library, the size of the workspace - is worked out once for each combination (the cached `_.._plan` functions); pointers are
@@ -36,6 +37,15 @@ def _refuse_devices(dev, **tensors):
 def _on(dev, *tensors):
     """Whether every given tensor is on the GPU `dev`: a pointer of another device would be read there."""
     return dev.type == "cuda" and all([t is None or t.device == dev for t in tensors])
+
+
+def _recorded(*tensors):
+    """Whether autograd would record what is done with these tensors."""
+    return torch.is_grad_enabled() and any([t is not None and t.requires_grad for t in tensors])
+
+
+def _refuse_gradients(call, instead):
+    raise ValueError(f"{call} gives no gradients, and a tensor requires one: {instead}detach it or call under torch.no_grad()")
 
 
 def _floats(name, t, n):
@@ -92,6 +102,8 @@ def group_norm(x, groups, gamma=None, beta=None, eps=1e-5, act="none", out=None)
     dev, shape, dtype = x.device, x.shape, x.dtype
     if not _on(dev, gamma, beta, out):
         _refuse_devices(dev, gamma=gamma, beta=beta, out=out)
+    if _recorded(x, gamma, beta, out):
+        _refuse_gradients("group_norm", "use group_norm_act, ")
     if out is None:
         out = _like(x)
     else:
@@ -113,6 +125,8 @@ def group_norm_backward(x, dy, mean, rstd, groups, gamma=None, beta=None, act="n
     dev, shape, dtype = x.device, x.shape, x.dtype
     if not _on(dev, dy, mean, rstd, gamma, beta):
         _refuse_devices(dev, dy=dy, mean=mean, rstd=rstd, gamma=gamma, beta=beta)
+    if _recorded(x, dy, mean, rstd, gamma, beta):
+        _refuse_gradients("group_norm_backward", "")
     _need(dy.shape == shape and dy.dtype == dtype, "dy: as x")
     dx = _like(x)
     plan, n = _norm_plan(shape, dtype, groups, act, 0.0, x.stride(), dx.stride(), dy.stride(), True)
@@ -191,6 +205,8 @@ def rotary(maps, positions, steps, axes=1, interleaved=False, magnitude=1.0, inv
     out = [_like(m) for m in maps] if out is None else list(out)
     if not _on(dev, positions, steps, *maps, *out):
         _refuse_devices(dev, positions=positions, steps=steps, **{f"maps[{i}]": m for i, m in enumerate(maps)}, **{f"out[{i}]": m for i, m in enumerate(out)})
+    if _recorded(*maps, *out):
+        _refuse_gradients("rotary", "use rotary_turn, ")
     _need(dtype in _DTYPE and all([m.dtype == dtype for m in (*maps, *out)]), "maps and out: float32, float16 or bfloat16, all of one type")
     hs = [_heads("the first map" if i == 0 else "the second map", x, y, shape) for i, (x, y) in enumerate(zip(maps, out))]
     _need(positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == shape[0] * axes, f"positions: {shape[0]} x {axes} contiguous int32 values")
@@ -264,6 +280,8 @@ class GpuCache:
         dev, shape = self.device, k.shape
         if not _on(dev, k, v, table, starts, held):
             _refuse_devices(dev, k=k, v=v, table=table, starts=starts, held=held)
+        if _recorded(k, v):
+            _refuse_gradients("store", "")
         _need(k.dtype == v.dtype and k.dtype in _DTYPE and v.shape == shape and len(shape) == 3 and shape[1:] == (self.heads, self.dim),
               f"k, v: [tokens, {self.heads}, {self.dim}] float32, float16 or bfloat16, of one type")
         c = self._cache(table)
@@ -294,6 +312,8 @@ class GpuCache:
         dev, shape = self.device, q.shape
         if not _on(dev, q, table, starts, lengths, mask, out):
             _refuse_devices(dev, q=q, table=table, starts=starts, lengths=lengths, mask=mask, out=out)
+        if _recorded(q, out):
+            _refuse_gradients("attend", "")
         _need(q.dtype in _DTYPE and len(shape) == 3 and shape[2] == self.dim, f"q: [tokens, q_heads, {self.dim}] float32, float16 or bfloat16")
         if out is None:
             out = _like(q)
