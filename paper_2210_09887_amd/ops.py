@@ -48,6 +48,11 @@ def _refuse_gradients(call, instead):
     raise ValueError(f"{call} gives no gradients, and a tensor requires one: {instead}detach it or call under torch.no_grad()")
 
 
+def _written(*tensors):
+    """Tells autograd that these tensors of the caller's hold other values now: what it saved of them is no longer there."""
+    torch.autograd.graph.increment_version(tensors)
+
+
 def _floats(name, t, n):
     _need(t is None or (t.dtype == torch.float32 and t.numel() == n and t.is_contiguous()), f"{name}: {n} contiguous float32 values")
 
@@ -104,10 +109,11 @@ def group_norm(x, groups, gamma=None, beta=None, eps=1e-5, act="none", out=None)
         _refuse_devices(dev, gamma=gamma, beta=beta, out=out)
     if _recorded(x, gamma, beta, out):
         _refuse_gradients("group_norm", "use group_norm_act, ")
-    if out is None:
-        out = _like(x)
-    else:
+    given = out is not None
+    if given:
         _need(out.shape == shape and out.dtype == dtype, "out: as x")
+    else:
+        out = _like(x)
     plan, n = _norm_plan(shape, dtype, groups, act, eps, x.stride(), out.stride())
     _floats("gamma", gamma, shape[3])
     _floats("beta", beta, shape[3])
@@ -117,6 +123,8 @@ def group_norm(x, groups, gamma=None, beta=None, eps=1e-5, act="none", out=None)
     rstd = torch.empty_like(mean)
     work = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
     _call(B.mdcnn_group_norm, dev, d, x.data_ptr(), out.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _ptr(work), n)
+    if given:
+        _written(out)
     return out, mean, rstd
 
 
@@ -202,7 +210,8 @@ def rotary(maps, positions, steps, axes=1, interleaved=False, magnitude=1.0, inv
     first = maps[0]
     shape, dev, dtype = first.shape, first.device, first.dtype
     _need(1 <= len(maps) <= 2 and (out is None or len(out) == len(maps)), "maps: one or two, out: as many")
-    out = [_like(m) for m in maps] if out is None else list(out)
+    given = out is not None
+    out = list(out) if given else [_like(m) for m in maps]
     if not _on(dev, positions, steps, *maps, *out):
         _refuse_devices(dev, positions=positions, steps=steps, **{f"maps[{i}]": m for i, m in enumerate(maps)}, **{f"out[{i}]": m for i, m in enumerate(out)})
     if _recorded(*maps, *out):
@@ -212,6 +221,8 @@ def rotary(maps, positions, steps, axes=1, interleaved=False, magnitude=1.0, inv
     _need(positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == shape[0] * axes, f"positions: {shape[0]} x {axes} contiguous int32 values")
     _need(steps.dtype == torch.int64 and steps.dim() == 1 and steps.is_contiguous(), "steps: contiguous int64 values of rotary_steps")
     _call(B.mdcnn_rotary, dev, hs, shape[0], shape[2], _DTYPE[dtype], positions.data_ptr(), axes, steps.data_ptr(), 2 * steps.numel(), interleaved, inverse, magnitude)
+    if given:
+        _written(*out)
     return out
 
 
@@ -288,6 +299,7 @@ class GpuCache:
         _per_sequence("starts", starts, c.n_seq + 1)
         _per_sequence("held", held, c.n_seq)
         _call(B.mdcnn_cache_store, dev, c, _heads("k", k, k, shape), _heads("v", v, v, shape), shape[0], starts.data_ptr(), held.data_ptr(), max_new, _DTYPE[k.dtype])
+        _written(self.k, self.v, self.k_scale, self.v_scale)
 
     def read(self, table, starts, first, max_new, tokens, dtype):
         """The values of tokens first[s] .. of every sequence s, starts[s + 1] - starts[s] of them, as (k, v) [tokens, heads, dim]; tokens = starts[-1]."""
@@ -315,10 +327,11 @@ class GpuCache:
         if _recorded(q, out):
             _refuse_gradients("attend", "")
         _need(q.dtype in _DTYPE and len(shape) == 3 and shape[2] == self.dim, f"q: [tokens, q_heads, {self.dim}] float32, float16 or bfloat16")
-        if out is None:
-            out = _like(q)
-        else:
+        given = out is not None
+        if given:
             _need(out.shape == shape and out.dtype == q.dtype, "out: as q")
+        else:
+            out = _like(q)
         c = self._cache(table)
         _per_sequence("starts", starts, c.n_seq + 1)
         _per_sequence("lengths", lengths, c.n_seq)
@@ -331,4 +344,6 @@ class GpuCache:
         work = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
         lse = torch.empty(shape[:2], dtype=torch.float32, device=dev)
         _call(B.mdcnn_cache_attend, dev, c, how, _heads("q", q, out, shape), _DTYPE[q.dtype], lse.data_ptr(), _ptr(work), n)
+        if given:
+            _written(out)
         return out, lse

@@ -51,3 +51,36 @@ def test_the_calls_for_autograd_take_them():
     q = torch.randn((3, 4, 16), device="cuda", requires_grad=True)
     (ops.group_norm_act(x, 2, act="silu").sum() + ops.rotary_turn((q,), ints([0, 1, 2]), ops.rotary_steps(16))[0].sum()).backward()
     assert x.grad is not None and q.grad is not None
+
+
+@pytest.mark.parametrize("name", ["group_norm", "rotary", "attend"])
+def test_autograd_knows_what_is_written_over(name):
+    """A tensor that a product has saved for its gradient, then written by the call."""
+    call, tensors = world()[name]
+    for kept in (False, True):
+        w = torch.ones_like(tensors["out"]).requires_grad_()
+        a = 2 * w
+        b = a * a
+        version = a._version
+        if not kept:
+            call(**{**tensors, "out": a.detach()})
+            assert a._version > version
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                b.sum().backward()
+        else:                                            # written elsewhere: the gradient is there
+            call(**tensors)
+            b.sum().backward()
+            assert torch.equal(w.grad, 8 * w.detach())
+
+
+def test_autograd_knows_that_a_store_writes_the_pages():
+    from paper_2210_09887_amd import ops
+    for mode in (torch.no_grad, torch.inference_mode):
+        with mode():
+            c = ops.GpuCache.empty(1, 2, 16)
+            x = torch.randn((3, 2, 16), device="cuda")
+            c.store(x, x, ints([[0]]), ints([0, 3]), ints([0]), 3)
+    c = ops.GpuCache.empty(1, 2, 16)
+    before = [t._version for t in (c.k, c.v, c.k_scale, c.v_scale)]
+    c.store(x.clone(), x.clone(), ints([[0]]), ints([0, 3]), ints([0]), 3)
+    assert all(t._version > n for t, n in zip((c.k, c.v, c.k_scale, c.v_scale), before))
