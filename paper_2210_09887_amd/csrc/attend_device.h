@@ -60,8 +60,9 @@ struct Rows {
         return true;
     }
     // positions that query i sees: lo <= position < hi
-    __device__ __forceinline__ int hi(const AttendJob& j, int i) const { return j.causal ? min(len, max(0, len - n + i + 1)) : len; }
-    __device__ __forceinline__ int lo(const AttendJob& j, int i) const { return j.window ? max(0, len - n + i + 1 - j.window) : 0; }
+    __device__ __forceinline__ int hi(const AttendJob& j, int i) const { return j.causal ? max(0, len - n + i + 1) : len; }
+    // (a window of any size: nothing negative less nothing negative)
+    __device__ __forceinline__ int lo(const AttendJob& j, int i) const { return j.window ? max(0, hi(j, i) - j.window) : 0; }
 };
 
 // Pages of the rows r0 .. r1 - 1 of a sequence, of which split z has the run [first, last).
@@ -69,7 +70,7 @@ struct Run {
     int first, last, splits;
     __device__ __forceinline__ Run(const AttendJob& j, const Rows& s, int r0, int r1, int z) {
         const int lo = s.lo(j, r0 / j.group), hi = s.hi(j, (r1 - 1) / j.group);
-        const int p0 = lo / MDCNN_PAGE_TOKENS, p1 = min((hi + MDCNN_PAGE_TOKENS - 1) / MDCNN_PAGE_TOKENS, j.max_pages);
+        const int p0 = lo / MDCNN_PAGE_TOKENS, p1 = min(hi / MDCNN_PAGE_TOKENS + (hi % MDCNN_PAGE_TOKENS > 0), j.max_pages);
         splits = max(0, (p1 - p0 + j.run - 1) / j.run);
         first = p0 + z * j.run;
         last = min(p1, first + j.run);
