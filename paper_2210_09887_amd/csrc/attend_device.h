@@ -84,20 +84,26 @@ constexpr float kRoom = 10.f, kUnroom = 1.f / 1024;
 constexpr float kSecond = 2048.f;
 constexpr _Float16 kSecondBack = (_Float16)(1.f / 2048);
 
-// The scale of a page's values in the exponent.  Its logarithm is rounded to 32 bits, which takes up to 2^-21 of the values; the inverse is that of the
-// rounded one, so that the sum of the exponentials does not notice.
-// The inverse takes kRoom out of the sum again.
+// The scale of a page's values in the exponent: log2 vs as a whole number and a part below one, 24 bits of it, so that a weight is as exact as its
+// logit whatever the size of the values.  What is left of that is in the weights of both sums: the inverse is the scale's own.
 struct ValueScale {
-    float log = 0.f, inverse = kUnroom;
+    float scale = 1.f;                                     // the page's, or the last one that could be used
     bool none = false, bad = false;                        // weights do not count in the sum of values; not a number
     __device__ __forceinline__ void next(float vs) {
         bad = vs != vs;
         none = vs < 7.8886090522101181e-31f;               // 2^-100; any scale does then: that of the page before
-        if (!none && !bad) {
-            log = __builtin_amdgcn_logf(vs);
-            inverse = exp2_fast(-log) * kUnroom;
-        }
+        if (!none && !bad) scale = vs;
+        asm volatile("" : "+v"(scale));                  // scalar registers are short in tiles of 256 channels
     }
+    __device__ __forceinline__ float whole() const { return (float)((int)(__float_as_uint(scale) >> 23) - 127); }
+    __device__ __forceinline__ float part() const { return __builtin_amdgcn_logf(__uint_as_float((__float_as_uint(scale) & 0x7fffffu) | 0x3f800000u)); }
+    __device__ __forceinline__ float inverse() const {
+        const float r = __builtin_amdgcn_rcpf(scale);
+        return __builtin_fmaf(__builtin_fmaf(-scale, r, 1.f), r, r);
+    }
+    __device__ __forceinline__ float log() const { return whole() + part(); }
+    // of the weights of a row: the exponent of a logit of zero
+    __device__ __forceinline__ float base(float top) const { return whole() + kRoom - (top == -INFINITY ? 0.f : top) + part(); }
 };
 
 // Factor of the products of a row with a page's keys.  Never zero: a hidden token's minus infinity stays that.

@@ -165,7 +165,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
             float add;
             half8 ph[2], pl[kTwo ? 2 : 1];
             auto weigh = [&]() {
-                const float base = val.log - (top == -INFINITY ? 0.f : top) + kRoom;
+                const float base = val.base(top);
                 float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int t = 0; t < 16; ++t) {
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
                 float m[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
                 for (int t = 4; t < 16; ++t) m[t % 4] = fmaxf(m[t % 4], x[t]);
-                const float most = max_over_32(max_over_16(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])))) * by + val.log;
+                const float most = max_over_32(max_over_16(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])))) * by + val.log();
                 const NextTop to(top, most, moves, values, valued);
                 top = to.top;
                 sum *= to.fade;
@@ -192,7 +192,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
                 for (int v = 0; v < NV; ++v) out[v] *= to.fade_out;
                 weigh();
             }
-            sum += add * val.inverse;
+            sum += add * kUnroom * val.inverse();
             if (val.bad) {
                 const bool bad = row_of_four(seen != 0, n);
 #pragma unroll

@@ -222,7 +222,7 @@ __global__ __launch_bounds__(kThreads, attend_tile_blocks(sizeof(T), DP)) void k
                 float add;
                 half8 ph[4], pl[kTwo ? 4 : 1];
                 auto weigh = [&]() {
-                    const float base = val.log - (top == -INFINITY ? 0.f : top) + kRoom;
+                    const float base = val.base(top);
                     float part[4];
 #pragma unroll
                     for (int t = 0; t < 32; ++t) {
@@ -242,7 +242,7 @@ __global__ __launch_bounds__(kThreads, attend_tile_blocks(sizeof(T), DP)) void k
                     float m[4] = {x[0][0], x[0][1], x[0][2], x[0][3]};
 #pragma unroll
                     for (int t = 4; t < 32; ++t) m[t % 4] = fmaxf(m[t % 4], x[t / 16][t % 16]);
-                    const float most = max_over_32(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]))) * by + val.log;
+                    const float most = max_over_32(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]))) * by + val.log();
                     const NextTop to(top, most, moves, values, valued);
                     top = to.top;
                     sum *= to.fade;
@@ -252,7 +252,7 @@ __global__ __launch_bounds__(kThreads, attend_tile_blocks(sizeof(T), DP)) void k
                         for (int i = 0; i < 16; ++i) out[d][i] *= to.fade_out;
                     weigh();
                 }
-                sum += add * val.inverse;
+                sum += add * kUnroom * val.inverse();
                 auto add_values = [&]() __attribute__((always_inline)) {
 #pragma unroll
                     for (int i = 0; i < 4 * ND; ++i) {

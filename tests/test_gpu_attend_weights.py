@@ -85,3 +85,26 @@ def test_weights_of_fp32_calls_keep_two_halves_of_bits(tokens, queries, copies, 
     for equal in (True, False):
         for sink_value in ("zero", "usual"):
             check_sink(tokens, queries, copies, gap, equal, sink_value, torch.float32, 2.0 ** -46)
+
+
+@pytest.mark.parametrize("size", [1e-27, 1e-20, 1e-9, 1.0, 1e9, 1e20, 1e33])
+@pytest.mark.parametrize("queries,pages", [(1, 1), (1, 7), (130, 1), (130, 7)])
+def test_values_of_any_size_keep_the_bits_of_fp32(queries, pages, size):
+    """All logits are zero: a result is the mean of codes times scales.  Its error: weights of 22 bits (4 * 2^-24), their exponent (16 beside the largest: 6) and
+    power (2), sums of 16 terms and over waves and pages (12), inverse and quotient (4); 32 * 2^-24 in all.  64 heads have scales of their own."""
+    from paper_2210_09887_amd import ops
+    g = torch.Generator().manual_seed(pages)
+    heads, n = 64, 64 * pages
+    c = ops.GpuCache.empty(pages, heads, DIM)
+    codes = torch.randint(20, 128, (pages, heads, DIM, PAGE), generator=g, dtype=torch.int8)
+    scale = torch.exp(2 * torch.rand((pages, heads), generator=g)) * size
+    c.k.fill_(0)
+    c.k_scale.fill_(1)
+    c.v.copy_(codes)
+    c.v_scale.copy_(scale)
+    out, lse = c.attend(torch.zeros((queries, heads, DIM), device="cuda"), ints([list(range(pages))]), ints([0, queries]), ints([n]), queries, n)
+    want = (codes.double() * scale.double()[..., None, None]).sum((0, 3)) / n
+    worst = float(((out.double().cpu() - want).abs() / want).max()) * 2 ** 24
+    print(f"{queries} queries, {pages} pages, values of {size:.0e}: {worst:.1f} * 2^-24", flush=True)
+    assert worst < 32
+    assert float((lse.double().cpu() - math.log(n)).abs().max()) < 32 * 2.0 ** -24 + 2.0 ** -24 * math.log(n) + 2.0 ** -24 * abs(math.log(size) - 10)
