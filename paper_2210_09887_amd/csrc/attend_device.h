@@ -112,8 +112,10 @@ __device__ __forceinline__ float factor_of(float logit, float ks) {
     return by < 1e-30f ? 1e-30f : by;
 }
 // T of a row is moved - and what has been summed faded - only where the weights of a lane add up to more than this (they have to be
-// halves, of which the largest is 65504, or finite where no values follow): weights are made before anyone looks for a maximum, and on nearly all pages no one does.
-constexpr float kMuch = 65504.f, kMuchNoValues = 18446744073709551616.f;
+// halves, of which the largest is 65504; where no values follow, what the sum takes of them has to stay below 2^110): weights are made
+// before anyone looks for a maximum, and on nearly all pages no one does.
+constexpr float kMuch = 65504.f;
+__device__ __forceinline__ float much(const ValueScale& val) { return val.none || val.bad ? fminf(val.scale * 0x1p120f, 0x1p127f) : kMuch; }
 
 // T of a row after a page whose largest x + log2 vs is `most` (minus infinity: the row sees none of it), and what the sums fade by.  The first page with
 // values sets it, whatever pages without values left (their sum is kept: no further down than that stays finite).

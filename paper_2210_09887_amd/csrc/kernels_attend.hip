@@ -178,7 +178,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
             };
             weigh();
             const bool values = !val.none && !val.bad;
-            bool moves = add > (values ? kMuch : kMuchNoValues) || (live && valued == 0.f);
+            bool moves = add > much(val) || (live && valued == 0.f);
             if (__any(moves)) {
                 moves = row_of_four(moves, n);
                 float m[4] = {x[0], x[1], x[2], x[3]};

@@ -236,7 +236,7 @@ __global__ __launch_bounds__(kThreads, attend_tile_blocks(sizeof(T), DP)) void k
                 };
                 weigh();
                 const bool values = !val.none && !val.bad;
-                bool moves = add > (values ? kMuch : kMuchNoValues) || (live && valued == 0.f);
+                bool moves = add > much(val) || (live && valued == 0.f);
                 if (__builtin_expect(__any(moves), 0)) {
                     moves = row_of_two(moves, n);
                     float m[4] = {x[0][0], x[0][1], x[0][2], x[0][3]};

@@ -108,3 +108,33 @@ def test_values_of_any_size_keep_the_bits_of_fp32(queries, pages, size):
     print(f"{queries} queries, {pages} pages, values of {size:.0e}: {worst:.1f} * 2^-24", flush=True)
     assert worst < 32
     assert float((lse.double().cpu() - math.log(n)).abs().max()) < 32 * 2.0 ** -24 + 2.0 ** -24 * math.log(n) + 2.0 ** -24 * abs(math.log(size) - 10)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("queries", [1, 130])
+@pytest.mark.parametrize("zeros_first", [False, True])
+@pytest.mark.parametrize("gap", [0.0, 10.0, 16.0, 20.0, 24.0, 30.0, 50.0, 80.0])
+def test_pages_of_zeros_above_values_as_small_as_they_count(gap, zeros_first, queries, dtype):
+    """Values of 2^-99 in the pages of one half, zeros with logits that lie `gap` higher in the other's: the sum of the exponentials stays finite, and right.
+    Errors: logits 8 * 2^-24 gap, sums over 8 pages and waves 32 * 2^-24, T of 100 in units of log 2, rounded with the log-sum: 2 * 2^-18."""
+    from paper_2210_09887_amd import ops
+    pages, n = 8, 512
+    c = ops.GpuCache.empty(pages, HEADS, DIM)
+    c.k.fill_(0)
+    c.v.fill_(100)
+    low, high = (slice(4, 8), slice(0, 4)) if zeros_first else (slice(0, 4), slice(4, 8))
+    c.k[high, :, :, 0] = 100
+    c.k_scale.fill_(0.01)
+    c.v_scale[low] = 2.0 ** -99
+    c.v_scale[high] = 0
+    q = torch.zeros((queries, HEADS, DIM))
+    q[..., 0] = gap * math.sqrt(DIM)
+    q = q.to(dtype)
+    out, lse = c.attend(q.cuda(), ints([list(range(pages))]), ints([0, queries]), ints([n]), queries, n)
+    real = float(q[0, 0, 0]) / math.sqrt(DIM)
+    total = 256 * (1 + math.exp(real))
+    assert float((lse.double().cpu() - math.log(total)).abs().max()) < (8 * gap + 32) * 2.0 ** -24 + 2 * 2.0 ** -18
+    # a result below 2^-126 may be anything down to zero
+    want = 100 * 2.0 ** -99 * 256 / total
+    u = 2.0 ** -24 if dtype == torch.float32 else 2.0 ** -8
+    assert float((out.double().cpu() - want).abs().max()) < want * (u + 2.0 ** -10 + 16 * gap * 2.0 ** -24) + 2.0 ** -126
