@@ -716,7 +716,7 @@ mdcnn_status mdcnn_cache_read(const mdcnn_cache_desc* c, const mdcnn_heads* k, c
  *   out = sum_j p_j v_j,  p = softmax over the tokens j that the query sees of scale q . k_j
  * A query sees every token of its sequence that has a page and, where a mask is given, a nonzero byte in it.  causal: query i of n is the token
  * lengths - n + i and sees nothing behind itself; window > 0 (causal only): only the `window` tokens up to itself.  A query that sees
- * nothing gets zeros and a log-sum of minus infinity; hidden tokens have no influence whatever their page holds.  Values of a page whose scale is
+ * nothing gets zeros and a log-sum of minus infinity, one that is not finite NaN wherever it sees a token; hidden tokens have no influence whatever their page holds.  Values of a page whose scale is
  * below 2^-100 count as zeros. */
 typedef struct {
     const int* starts_dev;    /* n_seq + 1                                              */

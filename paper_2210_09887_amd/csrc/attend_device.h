@@ -106,6 +106,10 @@ struct ValueScale {
     __device__ __forceinline__ float base(float top) const { return whole() + kRoom - (top == -INFINITY ? 0.f : top) + part(); }
 };
 
+// In place of a row's factor (which is not negative): its query is not finite.  It goes through as zeros, so that hidden tokens stay hidden, and its sum
+// becomes NaN at the end if it has seen any token.
+constexpr float kSpoiled = -1.f;
+
 // Factor of the products of a row with a page's keys.  Never zero: a hidden token's minus infinity stays that.
 __device__ __forceinline__ float factor_of(float logit, float ks) {
     const float by = logit * ks;

@@ -53,14 +53,19 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
     const T* q = (const T*)j.q + (s.q0 + (live ? query : 0)) * j.q_token + (long long)(head * j.group + (live ? row % j.group : 0)) * j.q_head;
     half8 qh[NS], ql[kTwo ? NS : 1];
     int e;
+    bool spoiled;
     {
-        float f[NS][8], top = 0.f;
+        float f[NS][8], top = 0.f, zero = 0.f;
 #pragma unroll
         for (int st = 0; st < NS; ++st) {
             eight_of(q, st < 2 * U ? 64 * (st / 2) + 16 * quad + 8 * (st & 1) : 64 * U + 8 * quad, live ? j.dim : 0, j.q_whole, f[st]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[st][i]));
+            for (int i = 0; i < 8; ++i) {
+                top = fmaxf(top, fabsf(f[st][i]));
+                zero = __builtin_fmaf(f[st][i], 0.f, zero);
+            }
         }
+        spoiled = row_of_four(zero != zero, n);
         top = max_over_32(max_over_16(top));
         e = exponent_of(top);
         const float sign = j.scale < 0.f ? -1.f : 1.f;
@@ -68,12 +73,12 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
         for (int st = 0; st < NS; ++st)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float x = scaled(f[st][i], -e) * sign;
+                const float x = spoiled ? 0.f : scaled(f[st][i], -e) * sign;
                 qh[st][i] = (_Float16)x;
                 if constexpr (kTwo) ql[st][i] = (_Float16)(x - (float)qh[st][i]);
             }
     }
-    const float logit = scaled(fabsf(j.scale) * kLog2E, e);      // (the queries have its sign)
+    const float logit = spoiled ? kSpoiled : scaled(fabsf(j.scale) * kLog2E, e);         // (the queries have its sign)
     const int hi = live ? s.hi(j, query) : 0, lo = live ? s.lo(j, query) : 0;
     const int all_hi = s.hi(j, r0 / j.group), all_lo = s.lo(j, (r1 - 1) / j.group);      // seen by every row
     const uint8_t* mask = j.mask ? j.mask + seq * j.mask_row : nullptr;
@@ -219,6 +224,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
         next = after;
         load_values(id);
     }
+    if (logit == kSpoiled && top > -INFINITY) sum = NAN;
     // join the four waves
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);

@@ -79,16 +79,21 @@ __global__ __launch_bounds__(kThreads, attend_tile_blocks(sizeof(T), DP)) void k
     half8 qh[kHeld], ql[kTwo ? NS : 1];
     half8* beyond = (half8*)(lds + 2 * S::kBytes) + threadIdx.x;
     int e;
+    bool spoiled;
     {
         const T* q = (const T*)j.q + (s.q0 + (live ? query : 0)) * j.q_token + (long long)(head * j.group + (live ? row % j.group : 0)) * j.q_head;
-        float top = 0.f;
+        float top = 0.f, zero = 0.f;
 #pragma unroll
         for (int st = 0; st < NS; ++st) {
             float f[8];
             eight_of(q, 16 * st + 8 * half, live ? j.dim : 0, j.q_whole, f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[i]));
+            for (int i = 0; i < 8; ++i) {
+                top = fmaxf(top, fabsf(f[i]));
+                zero = __builtin_fmaf(f[i], 0.f, zero);
+            }
         }
+        spoiled = row_of_two(zero != zero, n);
         top = max_over_32(top);
         e = exponent_of(top);
         const float sign = j.scale < 0.f ? -1.f : 1.f;
@@ -98,7 +103,7 @@ __global__ __launch_bounds__(kThreads, attend_tile_blocks(sizeof(T), DP)) void k
             eight_of(q, 16 * st + 8 * half, live ? j.dim : 0, j.q_whole, f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                f[i] = scaled(f[i], -e) * sign;
+                f[i] = spoiled ? 0.f : scaled(f[i], -e) * sign;
                 if constexpr (kTwo) ql[st][i] = (_Float16)(f[i] - (float)(_Float16)f[i]);
             }
             half8 h;
@@ -108,7 +113,7 @@ __global__ __launch_bounds__(kThreads, attend_tile_blocks(sizeof(T), DP)) void k
             else beyond[(st - kHeld) * kThreads] = h;
         }
     }
-    const float logit = scaled(fabsf(j.scale) * kLog2E, e);
+    const float logit = spoiled ? kSpoiled : scaled(fabsf(j.scale) * kLog2E, e);
     const int hi = live ? s.hi(j, query) : 0, lo = live ? s.lo(j, query) : 0;
     // of the wave's rows: what every one sees, what any one sees
     const int w0 = min(r0 + 32 * wave, s.rows - 1) / j.group, w1 = min(r0 + 32 * wave + 31, s.rows - 1) / j.group;
@@ -299,6 +304,7 @@ __global__ __launch_bounds__(kThreads, attend_tile_blocks(sizeof(T), DP)) void k
         next = after;
     }
     if (!live) return;
+    if (logit == kSpoiled && top > -INFINITY) sum = NAN;
     sum += __shfl_xor(sum, 32, 64);
     const bool whole = run.splits <= 1;
     const long long slot = ((((long long)seq * j.heads + head) * j.tiles + tile) * j.splits + split) * kAttendTile + 32 * wave + n;
