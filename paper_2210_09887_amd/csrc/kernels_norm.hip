@@ -29,18 +29,33 @@ __device__ __forceinline__ long long at_pixel(const mdcnn_strides& s, int p, int
     return flat ? (long long)p * s.x : (long long)(p / W) * s.y + (long long)(p % W) * s.x;
 }
 
-template <int ACT>
+// s = 1 / (1 + exp(-u)) and 1 - s.  Maps of fp32: from the exponential of -|u|, so that neither is a difference; of 16 bits: the exponent a rounded
+// product and 1 - s a difference, which take |u| 2^-24 of a value, far less than its own rounding.
+struct Sigmoid {
+    float s, rest;
+};
+template <typename T>
+__device__ __forceinline__ Sigmoid sigmoid_of(float u) {
+    if constexpr (sizeof(T) == 4) {
+        const float e = expf(-fabsf(u)), big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
+        return u < 0.f ? Sigmoid{small, big} : Sigmoid{big, small};
+    } else {
+        const float s = __builtin_amdgcn_rcpf(1.f + exp2_fast(-1.44269504f * u));
+        return {s, 1.f - s};
+    }
+}
+template <int ACT, typename T>
 __device__ __forceinline__ float act_of(float u) {
-    if (ACT == MDCNN_ACT_SILU) return u * __builtin_amdgcn_rcpf(1.f + exp2_fast(-1.44269504f * u));
+    if (ACT == MDCNN_ACT_SILU) return u * sigmoid_of<T>(u).s;
     if (ACT == MDCNN_ACT_RELU) return u < 0.f ? 0.f : u;
     return u;
 }
-// act'(u).  silu: s + u s (1 - s), s = 1 / (1 + exp(-u)); nothing of it overflows.
-template <int ACT>
+// act'(u).  silu: s + u s (1 - s); nothing of it overflows.
+template <int ACT, typename T>
 __device__ __forceinline__ float slope_of(float u) {
     if (ACT == MDCNN_ACT_SILU) {
-        const float s = __builtin_amdgcn_rcpf(1.f + exp2_fast(-1.44269504f * u));
-        return __builtin_fmaf(u * s, 1.f - s, s);
+        const Sigmoid g = sigmoid_of<T>(u);
+        return __builtin_fmaf(u * g.s, g.rest, g.s);
     }
     if (ACT == MDCNN_ACT_RELU) return u > 0.f ? 1.f : u == u ? 0.f : u;
     return 1.f;
@@ -199,7 +214,7 @@ struct Channels {
         float f[VEC];
         unpack(x, f);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) f[i] = act_of<ACT>(__builtin_fmaf(f[i] - mean[i], scale[i], beta[i]));
+        for (int i = 0; i < VEC; ++i) f[i] = act_of<ACT, T>(__builtin_fmaf(f[i] - mean[i], scale[i], beta[i]));
         return pack<T, VEC>(f);
     }
 };
@@ -223,7 +238,7 @@ struct GradChannels {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
             d[i] -= mean[i];
-            if (ACT != MDCNN_ACT_NONE) du[i] *= slope_of<ACT>(__builtin_fmaf(d[i], scale[i], beta[i]));
+            if (ACT != MDCNN_ACT_NONE) du[i] *= slope_of<ACT, T>(__builtin_fmaf(d[i], scale[i], beta[i]));
         }
     }
 };
