@@ -30,9 +30,13 @@ struct AttendBlock {
     }
 };
 
-template <typename T, int DP>
+// TWO: weights as two halves, 22 bits, else one, 11 bits.  fp32 calls always; 16-bit ones where sixteen rows are all there are, whose results are then those of weights in 32
+// bits rounded once.  One half / two, 16 bf16 sequences of 8192 tokens, 8 heads: 1 row of 64 channels 30.2 / 31.4 us, of 128 47.5 / 49.0, of 256 109 / 112;
+// 64 rows 65.9 / 82.1, 119 / 131, 297 / 329, more than the bits are worth: one half takes up to 2^-12 of a weight, fp16 results are off by 2.3e-4 of their norm
+// instead of 2.1e-4, bf16 ones by 1.7e-3 with either.
+template <typename T, int DP, bool TWO>
 __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(AttendJob j) {
-    constexpr bool kTwo = sizeof(T) == 4;                  // fp32 queries and probabilities as sums of two halves
+    constexpr bool kTwo = sizeof(T) == 4;                  // fp32 queries as sums of two halves
     constexpr int NS = DP / 32, NV = DP / 16;              // steps of 32 channels, tiles of 16
     constexpr int U = DP / 64;                             // pairs of steps that a 16-byte load serves
     __shared__ float s_top[kWaves][16], s_sum[kWaves][16];
@@ -168,7 +172,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
         if (by == by) {
             // weights, at first as if T stayed
             float add;
-            half8 ph[2], pl[kTwo ? 2 : 1];
+            half8 ph[2], pl[TWO ? 2 : 1];
             auto weigh = [&]() {
                 const float base = val.base(top);
                 float part[4] = {0.f, 0.f, 0.f, 0.f};
@@ -177,7 +181,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
                     const float w = exp2_fast(__builtin_fmaf(x[t], by, base));
                     part[t % 4] += w;
                     ph[t / 8][t % 8] = (_Float16)w;
-                    if constexpr (kTwo) pl[t / 8][t % 8] = (_Float16)((w - (float)ph[t / 8][t % 8]) * kSecond);
+                    if constexpr (TWO) pl[t / 8][t % 8] = (_Float16)((w - (float)ph[t / 8][t % 8]) * kSecond);
                 }
                 add = (part[0] + part[1]) + (part[2] + part[3]);
             };
@@ -210,7 +214,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
                     const half8 a = halves_of(vr[v][0], vr[v][1]), b = halves_of(vr[v][2], vr[v][3]);
                     out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, ph[0], out[v], 0, 0, 0);
                     out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, ph[1], out[v], 0, 0, 0);
-                    if constexpr (kTwo) {
+                    if constexpr (TWO) {
                         out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a * kSecondBack, pl[0], out[v], 0, 0, 0);
                         out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b * kSecondBack, pl[1], out[v], 0, 0, 0);
                     }
@@ -322,7 +326,9 @@ hipError_t launch_join(AttendJob j, hipStream_t st) {
 }
 template <typename T, int DP>
 hipError_t launch(const AttendJob& j, hipStream_t st) {
-    k_attend_rows<T, DP><<<(unsigned)((long long)j.splits * j.tiles * j.n_seq * j.heads), kThreads, 0, st>>>(j);
+    const unsigned blocks = (unsigned)((long long)j.splits * j.tiles * j.n_seq * j.heads);
+    if (sizeof(T) == 4 || j.tiles == 1) k_attend_rows<T, DP, true><<<blocks, kThreads, 0, st>>>(j);
+    else k_attend_rows<T, DP, sizeof(T) == 4><<<blocks, kThreads, 0, st>>>(j);
     return hipGetLastError();
 }
 struct Rows16 {

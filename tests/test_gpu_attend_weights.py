@@ -138,3 +138,29 @@ def test_pages_of_zeros_above_values_as_small_as_they_count(gap, zeros_first, qu
     want = 100 * 2.0 ** -99 * 256 / total
     u = 2.0 ** -24 if dtype == torch.float32 else 2.0 ** -8
     assert float((out.double().cpu() - want).abs().max()) < want * (u + 2.0 ** -10 + 16 * gap * 2.0 ** -24) + 2.0 ** -126
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("dim", [32, 128, 256])
+def test_few_queries_are_rounded_once(dim, dtype):
+    """Up to 16 rows: weights of 22 bits and sums in 32 leave (8 * 8 + 4 + 16) * 2^-24 of a result whose values are all positive, so that no more of
+    them lie on the wrong side of a rounding than twice that in units of the type."""
+    from paper_2210_09887_amd import ops
+    g = torch.Generator().manual_seed(dim)
+    seqs, n = 64, 5
+    c = ops.GpuCache.empty(seqs, HEADS, dim)
+    k = torch.randint(-127, 128, (seqs, HEADS, PAGE, dim), generator=g, dtype=torch.int8)
+    v = torch.randint(20, 128, (seqs, HEADS, dim, PAGE), generator=g, dtype=torch.int8)
+    c.k.copy_(k)
+    c.v.copy_(v)
+    c.k_scale.fill_(1 / 64)
+    c.v_scale.fill_(1 / 64)
+    q = torch.randn((seqs, HEADS, dim), generator=g).to(dtype)
+    out, _ = c.attend(q.cuda(), ints([[i] for i in range(seqs)]), ints(list(range(seqs + 1))), ints([n] * seqs), 1, n)
+    score = (k[:, :, :n].double() / 64 @ q.double()[..., None])[..., 0] * float(torch.tensor(dim ** -0.5))
+    assert float(score.abs().max()) < 8
+    want = (v[..., :n].double() / 64 @ torch.softmax(score, -1)[..., None])[..., 0]
+    wrong = float((out.cpu() != want.to(dtype)).double().mean())
+    bound = 2 * 84 * 2.0 ** -24 / EPS[dtype]
+    print(f"{dtype} {dim}: {wrong:.5f} of the results rounded the wrong way, bound {bound:.5f}", flush=True)
+    assert wrong < bound
