@@ -362,10 +362,9 @@ mdcnn_status mdcnn_rotary(const mdcnn_heads* maps, int n_maps, int tokens, int d
     // A thread goes through up to 16 heads with the same sines; fewer where that leaves less than eight blocks to a compute unit.  (40 bf16 heads of 128
     // channels: 32768 tokens 130 us, one head to a thread 147; 48 tokens 3.6 us, 16 heads to a thread 9.1.)
     const int heads = j.maps[0].heads + j.maps[1].heads;
-    const long long blocks = (tokens + j.tokens_per_block - 1) / j.tokens_per_block;
+    const long long blocks = ((long long)tokens + j.tokens_per_block - 1) / j.tokens_per_block;
     j.group = std::min(heads, 16);
-    while (j.group > 1 && blocks * ((heads + j.group - 1) / j.group) < 2048) j.group = (j.group + 1) / 2;
-    if (j.group == 1 && heads > 65535) j.group = 2;                        // (the grid's second extent)
+    while (j.group > 1 && blocks * ((heads + j.group - 1) / j.group) < 2048) j.group = (j.group + 1) / 2;      // (the second extent of the grid is 8192 at most)
     return launched(launch_rotary(j, dtype, vec, interleaved != 0, (hipStream_t)stream), "rotary");
 }
 
