@@ -79,7 +79,7 @@ struct Run {
 
 // Where weights lie: the largest that T knows at 2^kRoom.  32 of them in a lane (a page of the tiles) add up to 2^15 then, below kMuch.
 constexpr float kRoom = 10.f, kUnroom = 1.f / 1024;
-// Weights as two halves: the second one holds 2^11 times what the first leaves, or it would end where the first does, and is multiplied with codes by 2^-11
+// Weights of fp32 calls as two halves: the second one holds 2^11 times what the first leaves, or it would end where the first does, and is multiplied with codes by 2^-11
 // (exact: they are whole numbers up to 127).
 constexpr float kSecond = 2048.f;
 constexpr _Float16 kSecondBack = (_Float16)(1.f / 2048);

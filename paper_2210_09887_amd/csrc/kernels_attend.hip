@@ -31,9 +31,10 @@ struct AttendBlock {
 };
 
 // TWO: weights as two halves, 22 bits, else one, 11 bits.  fp32 calls always; 16-bit ones where sixteen rows are all there are, whose results are then those of weights in 32
-// bits rounded once.  One half / two, 16 bf16 sequences of 8192 tokens, 8 heads: 1 row of 64 channels 30.2 / 31.4 us, of 128 47.5 / 49.0, of 256 109 / 112;
-// 64 rows 65.9 / 82.1, 119 / 131, 297 / 329, more than the bits are worth: one half takes up to 2^-12 of a weight, fp16 results are off by 2.3e-4 of their norm
-// instead of 2.1e-4, bf16 ones by 1.7e-3 with either.
+// bits rounded once.  One half / two, 16 bf16 sequences of 8192 tokens, 8 heads: 1 row of 64 channels 30.2 / 31.5 us, of 128 47.5 / 48.0, of 256 109 / 111;
+// 64 rows 63.5 / 77.6, 118 / 123, 294 / 319, more than the bits are worth: one half takes up to 2^-12 of a weight, fp16 results are off by 2.3e-4 of their norm
+// instead of 2.1e-4, bf16 ones by 1.7e-3 with either.  The second half of 16-bit calls is what the first leaves, 2^-35 of the largest weight at its finest; in fp32
+// calls 2^11 times that (attend_device.h).
 template <typename T, int DP, bool TWO>
 __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(AttendJob j) {
     constexpr bool kTwo = sizeof(T) == 4;                  // fp32 queries as sums of two halves
@@ -181,7 +182,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
                     const float w = exp2_fast(__builtin_fmaf(x[t], by, base));
                     part[t % 4] += w;
                     ph[t / 8][t % 8] = (_Float16)w;
-                    if constexpr (TWO) pl[t / 8][t % 8] = (_Float16)((w - (float)ph[t / 8][t % 8]) * kSecond);
+                    if constexpr (TWO) pl[t / 8][t % 8] = (_Float16)((w - (float)ph[t / 8][t % 8]) * (kTwo ? kSecond : 1.f));
                 }
                 add = (part[0] + part[1]) + (part[2] + part[3]);
             };
@@ -215,8 +216,8 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_rows(Att
                     out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, ph[0], out[v], 0, 0, 0);
                     out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, ph[1], out[v], 0, 0, 0);
                     if constexpr (TWO) {
-                        out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a * kSecondBack, pl[0], out[v], 0, 0, 0);
-                        out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b * kSecondBack, pl[1], out[v], 0, 0, 0);
+                        out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kTwo ? a * kSecondBack : a, pl[0], out[v], 0, 0, 0);
+                        out[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kTwo ? b * kSecondBack : b, pl[1], out[v], 0, 0, 0);
                     }
                     if (v % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }

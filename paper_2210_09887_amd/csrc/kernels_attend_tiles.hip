@@ -7,8 +7,8 @@
 // What bounds it is the issue of vector instructions beside the matrix ones (an exponential, a product and sum, a sum and half a conversion for each weight, ten
 // to make eight codes halves): counted together they fill a SIMD's time.  4 x 4096 queries of 32 bf16 heads of 128 channels over 8 and 8192 tokens
 // 2.3 ms, 950 TFLOP/s (64 channels 1.45 ms, 760; 32 channels, 16 x 2048 queries of 8 heads, 0.62 ms, 445).
-// Weights of 16-bit calls are one half: it takes up to 2^-12 of each, and fp16 results of 32 channels are off by 2.3e-4 of their norm instead of 2.1e-4, bf16 ones by 1.7e-3 with either.  As
-// two halves, like those of fp32 calls, 2 x 1728 pixels over 13824 tokens of 8 heads of 32 would take 211 us instead of 150, three prompts of 128 channels 937 instead of 662.
+// Weights of 16-bit calls are one half: it takes up to 2^-12 of each, and fp16 results of 32 channels are off by 2.3e-4 of their norm instead of 2.1e-4, bf16 ones by 1.7e-3 with either.
+// As two halves 2 x 1728 pixels over 13824 tokens of 8 heads of 32 would take 191 us instead of 149, three prompts of 128 channels 909 instead of 680.
 // Rows of LDS are 16-byte chunks that are permuted by their row (chunk ^ row), so that neither the reads of 16 rows side by side nor the
 // writes meet in a bank.
 #include "attend_device.h"
