@@ -234,14 +234,17 @@ mdcnn_status check_attend(const mdcnn_cache_desc* c, const mdcnn_attend_desc* a,
     return MDCNN_OK;
 }
 
-// Rows to a block and pages to a split.  Up to 64 rows go by sixteen, blocks that each read the cache (from the second on mostly out of the L2); more by 128,
-// whose codes are read once and made halves once.  16 sequences of 8192 tokens, 8 heads of 128 channels, by sixteen / by 128: 16 rows 50 / 104 us,
-// 48 rows 103 / 135, 64 rows 122 / 139, 128 rows 233 / 193; 64 of 1024 tokens, 64 channels: 64 rows 43 / 48, 128 rows 79 / 66.
+// Rows to a block and pages to a split.  Up to 16 rows go by sixteen, whose blocks read the cache's bytes and little else, more than 64 by 128, whose codes are read once and made halves
+// once; 17 to 64 by sixteen - two to four blocks that each read and decode - but for heads of 64 to 128 channels of 16 bits as soon as those are more than the 1024 blocks that
+// fill the GPU twice (of 32 channels a tile's own work is the longer, of 192 and more or of fp32 there is one tile to a compute unit).  By sixteen / by 128, us, 8 bf16 heads:
+//   128 channels: 16 x 8192 tokens, 16 rows 50 / 72, 48 rows 102 / 85, 64 rows 118 / 87, 128 rows 225 / 114; 64 x 8192, 32 rows 383 / 224, 64 rows 830 / 284; 2 x 30000, 48 rows 50 / 52;
+//   1 x 2000, 48 rows 18 / 26.  64 channels: 16 x 8192, 32 rows 37 / 42, 64 rows 60 / 54; 64 x 1024, 64 rows 43 / 35.  32 channels: 64 x 8192, 48 rows 123 / 160.
+//   256 channels: 16 x 8192, 48 rows 246 / 331.  fp32, 128 channels: 16 x 8192, 64 rows 140 / 181.
 // Runs of 12 to 32 pages by sixteen rows: shorter ones are mostly what a block does once (its queries, its sums: two sequences of 150001 tokens, 2 heads,
-// 60 us with 4 pages, 45 with 8, 37 with 24), longer ones leave the last blocks of ragged sequences alone on the GPU; in between just under the 512 blocks that
+// 63 us with 4 pages, 46 with 8, 36 with 24), longer ones leave the last blocks of ragged sequences alone on the GPU; in between just under the 512 blocks that
 // the GPU holds.  By 128 rows as many runs as the GPU holds blocks, but none shorter than 8 pages: a run leaves its sums in 32 bits, and one that begins when others
-// end leaves the GPU half empty (against about 2048 blocks: prompt of 2000 tokens, 32 heads of 128 channels over 8, 90 and 140 us; two prompts of 1300
-// and 700 behind 4000 and 2000, 64 channels, 85 and 94; 1000 rows over 8192 tokens, 8 heads of 128 channels, 105 and 110).
+// end leaves the GPU half empty (against about 2048 blocks: prompt of 2000 tokens, 32 heads of 128 channels over 8, 81 and 134 us; 1000 rows over 8192 tokens, 8
+// heads of 128 channels, 76 and 100).
 mdcnn_status plan_attend(const mdcnn_cache_desc& c, const mdcnn_attend_desc& a, int q_heads, int dtype, AttendJob& j, size_t* bytes) {
     j.pages = c.pages; j.heads = c.heads; j.group = q_heads / c.heads; j.dim = c.dim; j.pitch = mdcnn_cache_pitch(c.dim);
     j.n_seq = c.n_seq; j.max_pages = c.pages ? c.max_pages : 0;
@@ -249,19 +252,25 @@ mdcnn_status plan_attend(const mdcnn_cache_desc& c, const mdcnn_attend_desc& a, 
     j.causal = a.causal; j.window = a.window; j.scale = a.scale;
     const long long rows = (long long)j.max_new * j.group;
     if (rows > 0x7fffff00ll || rows * c.n_seq * c.heads > 0x7fffffffll) return fail(MDCNN_ERR_SIZE, "cache_attend: too many rows");
-    j.tile_rows = rows <= 64 || !attend_tiles_fit(dtype, j.pitch) ? kAttendRows : kAttendTile;
-    j.tiles = (int)((rows + j.tile_rows - 1) / j.tile_rows);
-    const long long columns = (long long)j.tiles * c.n_seq * c.heads;
-    const long long live = std::min(columns, ((long long)j.tokens * j.group / j.tile_rows + c.n_seq) * c.heads);        // (no more of them have rows)
     long long most = std::min<long long>((a.max_len + (long long)MDCNN_PAGE_TOKENS - 1) / MDCNN_PAGE_TOKENS, c.max_pages);
     if (a.window) most = std::min<long long>(most, (a.window + (long long)j.max_new + 2 * MDCNN_PAGE_TOKENS - 2) / MDCNN_PAGE_TOKENS);
     most = std::max(most, 1ll);
-    if (j.tile_rows == kAttendRows) {
-        const long long run = std::min(32ll, std::max(12ll, (most * live + 479) / 480));
-        j.splits = live >= 2048 ? 1 : (int)((most + run - 1) / run);
-    } else {
-        j.splits = (int)std::max(1ll, std::min((most + 7) / 8, 256ll * attend_tile_blocks((int)storage_bytes(dtype), j.pitch) / std::max(1ll, live)));
-    }
+    long long columns, live;
+    auto cut = [&](int tile_rows) {
+        j.tile_rows = tile_rows;
+        j.tiles = (int)((rows + tile_rows - 1) / tile_rows);
+        columns = (long long)j.tiles * c.n_seq * c.heads;
+        live = std::min(columns, ((long long)j.tokens * j.group / tile_rows + c.n_seq) * c.heads);        // (no more of them have rows)
+        if (tile_rows == kAttendRows) {
+            const long long run = std::min(32ll, std::max(12ll, (most * live + 479) / 480));
+            j.splits = live >= 2048 ? 1 : (int)((most + run - 1) / run);
+        } else {
+            j.splits = (int)std::max(1ll, std::min((most + 7) / 8, 256ll * attend_tile_blocks((int)storage_bytes(dtype), j.pitch) / std::max(1ll, live)));
+        }
+    };
+    cut(kAttendRows);
+    const bool lean = storage_bytes(dtype) == 2 && j.pitch >= 64 && j.pitch <= 128;
+    if (attend_tiles_fit(dtype, j.pitch) && (rows > 64 || (rows > 16 && lean && live * j.splits > 1024))) cut(kAttendTile);
     j.run = j.splits == 1 ? 1 << 30 : (int)((most + j.splits - 1) / j.splits);          // all alike
     if (columns * j.splits > 0x7fffffffll) return fail(MDCNN_ERR_SIZE, "cache_attend: too large");
     *bytes = j.splits > 1 ? (size_t)columns * j.splits * j.tile_rows * (8 + 4 * (size_t)j.pitch) + 256 : 0;

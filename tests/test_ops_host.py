@@ -171,3 +171,12 @@ def test_a_cache_without_pages_or_a_table_without_entries_needs_no_memory(kw):
     refused(4, B.mdcnn_cache_attend, cache(**kw), attending(), heads(heads=8, x_token=256, y_token=256), 1, FAKE + 2, None, 0)
     for call in (B.mdcnn_cache_store, B.mdcnn_cache_read):
         refused(1, call, cache(**kw), heads(), heads(), 3, None, FAKE, 3, 1)
+
+
+def test_few_rows_of_many_long_sequences_go_by_the_tile():
+    """32 to 64 rows of 64 sequences of 8192 tokens: tiles fill the GPU without splits, so nothing is left to be joined; two sequences are split, and so are rows of 32 channels."""
+    def need(dim, n_seq, rows, dtype=1):
+        c, a = cache(dim=dim, n_seq=n_seq, heads=8, max_pages=128, pages=9000), attending(tokens=n_seq * rows, max_new=rows, max_len=8192)
+        return B.mdcnn_cache_attend_bytes(c, a, 8, dtype)
+    assert need(128, 64, 48) == need(96, 64, 32) == need(128, 64, 64) == 0
+    assert need(128, 2, 64) > 0 and need(32, 16, 64) > 0 and need(128, 16, 16) > 0 and need(128, 16, 64, 0) > 0
