@@ -8,7 +8,7 @@
 //
 // Codes become halves without a conversion: a byte c + 128 in the low byte of 0x6400 is the half 1152 + c, minus 1152 is c,
 // exactly.  The scale of a page's keys is multiplied into the logits.  That of its values goes into the exponent,
-//   w = 2^(x + log2 vs - T + kRoom),  T the row's largest x + log2 vs so far,
+//   w = 2^(x + log2 vs - T + kRoom),  T the row's largest x + log2 vs when it was last moved,
 // so that w is a half next to what counts most in this row, whatever the sizes of scales and values: sum w code / sum (w / vs) is the result,
 // 2^(T - kRoom) sum (w / vs) the sum of the exponentials.  Weights near 2^kRoom at the top leave the halves' range to those below: one has all its bits
 // down to 2^-24 of the largest, and a step of 2^-34 of it from there (a first token 14 above 4096 others: with the largest at 1 the others' part of the result

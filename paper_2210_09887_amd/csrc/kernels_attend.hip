@@ -5,8 +5,8 @@
 // them; the next page's keys are on their way while the softmax and the values of this one are worked on, and the other way
 // round.  A wave has pages of its own (every fourth of its block's run) with a maximum and a sum of its own; the four are joined
 // in LDS.  Runs of pages are split over blocks where rows alone would not fill the GPU, and joined by a second launch.
-// One bf16 token of 32 heads over 8 for each of 48 sequences of 1 to 16384 tokens (193 MB) 50-55 us, 3.7 TB/s (the longest sequences end last), and 4.5 to join;
-// two sequences of 150001 tokens, 2 heads (154 MB) 28 us, 5.4 TB/s, and 6 to join; 700 tokens of fp32 8 us.
+// One bf16 token of 32 heads over 8 for each of 48 sequences of 1 to 16384 tokens (193 MB) 51-54 us, 3.6 TB/s (the longest sequences end last), and 5 to join;
+// two sequences of 150001 tokens, 2 heads (154 MB) 28 us, 5.4 TB/s, and 6 to join; 700 tokens of fp32 9 us.
 #include "attend_device.h"
 
 namespace mdcnn {

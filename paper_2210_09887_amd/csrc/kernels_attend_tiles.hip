@@ -5,8 +5,8 @@
 // queries (v_mfma_f32_32x32x16_f16, the queries stay in registers), the weights, as many products with the values; the weights need not leave
 // the registers they come to be in (attend_device.h).
 // What bounds it is the issue of vector instructions beside the matrix ones (an exponential, a product and sum, a sum and half a conversion for each weight, ten
-// to make eight codes halves): counted together they fill a SIMD's time.  4 x 4096 queries of 32 bf16 heads of 128 channels over 8 and 8192 tokens
-// 2.3 ms, 950 TFLOP/s (64 channels 1.45 ms, 760; 32 channels, 16 x 2048 queries of 8 heads, 0.62 ms, 445).
+// to make eight codes halves): 56 and 39 % of the busy time with 128 channels.  4 x 4096 queries of 32 bf16 heads of 128 channels over 8 and 8192 tokens
+// 2.35 ms, 935 TFLOP/s (64 channels 1.36 ms, 805; 32 channels, 16 x 2048 queries of 8 heads, 0.52 ms, 530).
 // Weights of 16-bit calls are one half: it takes up to 2^-12 of each, and fp16 results of 32 channels are off by 2.3e-4 of their norm instead of 2.1e-4, bf16 ones by 1.7e-3 with either.
 // As two halves 2 x 1728 pixels over 13824 tokens of 8 heads of 32 would take 191 us instead of 149, three prompts of 128 channels 909 instead of 680.
 // Rows of LDS are 16-byte chunks that are permuted by their row (chunk ^ row), so that neither the reads of 16 rows side by side nor the
@@ -52,7 +52,7 @@ __device__ __forceinline__ void ahead_of() {
 __device__ __forceinline__ void page_over() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // More waves to a SIMD help: one wave issues a vector instruction every five
-// cycles, two or three together one every three.  (64 channels of 16 bits: two waves 1744 us for 4 x 4096 queries of 32 heads over 8192 tokens, three 1602.)
+// cycles, two or three together one every three.  (64 channels of 16 bits: two waves 1468 us for 4 x 4096 queries of 32 heads over 8192 tokens, three 1360.)
 template <typename T, int DP, bool MASK>
 __global__ __launch_bounds__(kThreads, attend_tile_blocks(sizeof(T), DP)) void k_attend_tiles(AttendJob j) {
     constexpr bool kTwo = sizeof(T) == 4;
